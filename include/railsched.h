@@ -20,7 +20,8 @@
  *     asynchronously on it; no call but railsched_check_capacity synchronises the host with the device.
  *   - Every function returns 0 (RAILSCHED_OK) or a negative railsched_status.  Arguments are
  *     validated on the host before anything is launched; on an error nothing has been enqueued.
- *   - All outputs are integers and are defined bit-exactly.
+ *   - All outputs are integers and are defined bit-exactly, but for those of the operators on a router in training
+ *     (railsched_route_logprobs, _balance, _distill and their gradients), which are defined by formulas.
  *   - Capacity.  Every call that reads or writes the per-chunk arrays (chunk_w, chunk_flow, perm, rail, port) takes
  *     `capacity`, the number of records those arrays hold.  The chunk count chunk_off[batch*M] exists on the device
  *     only; when it exceeds `capacity` the call touches none of the per-chunk arrays and fills its remaining outputs
@@ -292,6 +293,100 @@ size_t railsched_port_round_robin_workspace_bytes(int32_t batch, const railsched
 int railsched_port_round_robin(const int64_t *chunk_off, const uint8_t *rail, int32_t batch,
                                const railsched_topo_t *h_topo, int32_t ports, int64_t capacity, uint8_t *port,
                                void *ws, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Operators on the logits of a router in training (the "Gate" of Algorithm 1 step 1).  They read the same rows of
+ * logits as stage 1 and, like stage 2, its picks; their outputs are floating point and are defined by the formulas
+ * below, evaluated in fp32 (sums over rows in fp32 per part and in fp64 over the parts), with one rounding to the
+ * type of the logits where a gradient has that type.  The order of every sum is fixed: equal inputs give equal bits.
+ *
+ * Common to all of them:
+ *   logits    rows of E values of type `dtype` (railsched_dtype), row r at logits + r*ld elements, ld >= E    (in)
+ *             A logit may be -infinity: that expert is out for this row (probability 0).  A row with NaN or
+ *             +infinity makes NaN of the floating outputs it enters and of no others.
+ *   row_mask  [rows] uint8, NULL = all rows count.  A row whose entry is 0 (padding) does not count, and neither does a
+ *             row whose logits are all -infinity: its logits (if masked) are not read, its picks are not counted, its
+ *             floating outputs and its gradient are 0, its alternatives -1.
+ *   temperature  tau > 0, finite: z = logits / tau, p = softmax(z) over the row, lse = log sum exp z.
+ *   d_logits  the gradient, type `dtype`, row r at d_logits + r*ld_d, ld_d >= E; not the same memory as logits.  Places
+ *             between the rows are left as they are.  accumulate = 0: overwritten; 1: added to what is there (each
+ *             sum rounded to `dtype`; rows that do not count are left as they are).
+ *   An index outside [0,E) is ignored.
+ * Limits: E <= 1024, k, m and K <= E, m and K <= 64, rows < 2^31, ld and ld_d <= 2^31.  rows may be 0 (nothing is written but the groups' outputs).
+ * Errors: NULL_PTR, INVALID_ARG (sizes, ld < E, unknown dtype, temperature not positive and finite, accumulate not 0 or 1,
+ * d_logits == logits), UNSUPPORTED (limits), WORKSPACE.
+ * ------------------------------------------------------------------------------------------- */
+typedef enum railsched_dtype { RAILSCHED_F32 = 0, RAILSCHED_BF16 = 1, RAILSCHED_F16 = 2 } railsched_dtype;
+
+/* Log probabilities of given experts, with log-sum-exp, entropy and the most likely experts of every row.
+ *   topk_idx  [rows][k] int32: the experts asked for (stage 1's picks, or another router's); NULL iff k == 0   (in)
+ *   logp      [rows][k] fp32: z[topk_idx] - lse; exp(logp) is the gate weight of the pick; 0 where ignored      (out)
+ *   lse       [rows] fp32                                                                                     (out, nullable)
+ *   entropy   [rows] fp32: -sum p log p                                                                       (out, nullable)
+ *   alt_idx   [rows][m] int32: the experts of the m largest logits in stage 1's order; -1 where fewer are left (out; NULL iff m == 0)
+ *   alt_logp  [rows][m] fp32: their z - lse; -infinity where alt_idx is -1 in a row that counts               (out; NULL iff m == 0)
+ * The logits of a row are read once; the picks' logits are fetched from the cache. */
+int railsched_route_logprobs(const void *logits, int32_t dtype, int64_t rows, int32_t E, int64_t ld, float temperature,
+                             const uint8_t *row_mask, const int32_t *topk_idx, int32_t k, int32_t m, float *logp, float *lse,
+                             float *entropy, int32_t *alt_idx, float *alt_logp, void *stream);
+
+/* Its gradient: d_logits[e] = (sum over slots j of e of d_logp[j] - p_e (sum over slots of d_logp - d_lse
+ * + d_entropy (log p_e + entropy))) / tau.  d_lse carries a loss on lse (its square: the z-loss).
+ *   d_logp [rows][k], d_lse [rows], d_entropy [rows] fp32 (in, each nullable = 0; d_logp NULL if k == 0) */
+int railsched_route_logprobs_backward(const void *logits, int32_t dtype, int64_t rows, int32_t E, int64_t ld, float temperature,
+                                      const uint8_t *row_mask, const int32_t *topk_idx, int32_t k, const float *d_logp,
+                                      const float *d_lse, const float *d_entropy, int32_t accumulate, void *d_logits, int64_t ld_d,
+                                      void *stream);
+
+/* Balance loss of groups of rows (layers, sequences, micro-batches), with the counts of picks per expert.  Group g
+ * holds the rows [group_off[g], group_off[g+1]), or with group_off NULL the g-th of `groups` equal parts of the rows.
+ * With n its rows that count, c_e its picks of expert e and P_e the sum of p_e over its rows that count:
+ *   loss[g] = coef * E / (k n^2) * sum_e c_e P_e        (0 if n == 0; temperature 1)
+ * which is coef where picks and probabilities are spread evenly.
+ *   group_off [groups+1] int64, not decreasing, within [0, rows]; nullable      (in; values outside are clamped)
+ *   topk_idx  [rows][k] int32                                                   (in)
+ *   counts    [groups][E] int64: c_e                                            (out)
+ *   tokens    [groups] int64: n                                                 (out)
+ *   prob_sum  [groups][E] fp32: P_e                                             (out)
+ *   loss      [groups] fp32                                                     (out)
+ *   ws        railsched_route_balance_workspace_bytes(rows, groups, E) bytes, 256-byte aligned
+ * Errors as above, also INVALID_ARG where group_off is NULL and rows is not a multiple of groups, groups < 0, k < 1. */
+size_t railsched_route_balance_workspace_bytes(int64_t rows, int32_t groups, int32_t E);
+int railsched_route_balance(const void *logits, int32_t dtype, int64_t rows, int32_t E, int64_t ld, const uint8_t *row_mask,
+                            const int32_t *topk_idx, int32_t k, const int64_t *group_off, int32_t groups, float coef,
+                            int64_t *counts, int64_t *tokens, float *prob_sum, float *loss, void *ws, size_t ws_bytes, void *stream);
+
+/* Its gradient through the probabilities (the counts are constants): with a_e = d_loss[g] coef E c_e / (k n^2),
+ * d_logits[e] = p_e (a_e - sum_f a_f p_f).  counts and tokens are inputs: a caller that adds them up over ranks first trains on
+ * the balance of all of them.  Rows of no group are left as they are.
+ *   counts [groups][E] int64, tokens [groups] int64, d_loss [groups] fp32       (in) */
+int railsched_route_balance_backward(const void *logits, int32_t dtype, int64_t rows, int32_t E, int64_t ld, const uint8_t *row_mask,
+                                     int32_t k, const int64_t *group_off, int32_t groups, float coef, const int64_t *counts,
+                                     const int64_t *tokens, const float *d_loss, int32_t accumulate, void *d_logits, int64_t ld_d,
+                                     void *stream);
+
+/* Distillation: the divergence of a router from the top logits of another one (the teacher), so that a forecaster of the
+ * routing can be trained before it feeds stage 1.  The teacher's list of a row is (t_idx[j], t_logit[j]), j < K; an entry
+ * with an index outside [0,E) or the logit -infinity is absent.  Its probabilities are
+ *   without t_lse: q = softmax(t_logit / tau) over the list;
+ *   with t_lse:    q = exp(t_logit / tau - t_lse), t_lse the teacher's log-sum-exp over all its experts at this temperature, and the
+ *                  rest q_r = max(0, 1 - sum q) is held against p_r, the sum of p outside the list (left out where p_r is 0).
+ *   loss[r] = tau^2 (sum_j q_j (log q_j - log p[t_idx[j]]) + q_r (log q_r - log p_r))
+ * A row without entries has the loss 0 (also with t_lse).  +infinity where q_j > 0 meets an expert that is out.
+ * An expert listed twice counts with the sum of its entries' terms.
+ *   t_idx [rows][K] int32, t_logit [rows][K] fp32, t_lse [rows] fp32 (nullable)  (in; alt_idx and alt_logp of railsched_route_logprobs
+ *                                                                                will do, with t_lse = 0 at temperature 1)
+ *   loss  [rows] fp32                                                            (out) */
+int railsched_route_distill(const void *logits, int32_t dtype, int64_t rows, int32_t E, int64_t ld, float temperature,
+                            const uint8_t *row_mask, const int32_t *t_idx, const float *t_logit, const float *t_lse, int32_t K,
+                            float *loss, void *stream);
+
+/* Its gradient: with Q = sum q, d_logits[e] = tau d_loss (p_e (Q + q_r) - sum over entries of e of q) in the list and
+ * tau d_loss p_e (Q + q_r - q_r / p_r) outside (without t_lse, or where p_r is 0: q_r = 0).
+ *   d_loss [rows] fp32 (in) */
+int railsched_route_distill_backward(const void *logits, int32_t dtype, int64_t rows, int32_t E, int64_t ld, float temperature,
+                                     const uint8_t *row_mask, const int32_t *t_idx, const float *t_logit, const float *t_lse, int32_t K,
+                                     const float *d_loss, int32_t accumulate, void *d_logits, int64_t ld_d, void *stream);
 
 #ifdef __cplusplus
 }

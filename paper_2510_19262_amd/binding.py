@@ -26,6 +26,9 @@ EXPORTS = (
     "railsched_lpt_spray_chunkwise",
     "railsched_eval_workspace_bytes", "railsched_eval", "railsched_schedule_workspace_bytes", "railsched_schedule", "railsched_schedule_static", "railsched_transpose_matrix", "railsched_assign_policy",
     "railsched_port_round_robin_workspace_bytes", "railsched_port_round_robin",
+    "railsched_route_logprobs", "railsched_route_logprobs_backward",
+    "railsched_route_balance_workspace_bytes", "railsched_route_balance", "railsched_route_balance_backward",
+    "railsched_route_distill", "railsched_route_distill_backward",
 )
 
 
@@ -73,7 +76,7 @@ def load():
     lib.railsched_version.restype = C.c_char_p
     lib.railsched_strerror.restype = C.c_char_p
     lib.railsched_strerror.argtypes = [C.c_int]
-    P, I32, I64, SZ = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
+    P, I32, I64, SZ, F32 = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t, C.c_float
     TP = C.POINTER(_TopoStruct)
     lib.railsched_route_topk.argtypes = [P, I64, I32, I32, P, P]
     lib.railsched_check_capacity.argtypes = [P, I32, TP, I64, C.POINTER(C.c_int64), P]
@@ -109,6 +112,17 @@ def load():
     for fn in ("railsched_check_capacity", "railsched_route_topk", "railsched_traffic_matrix", "railsched_route_traffic",
                "railsched_chunk_sort", "railsched_lpt_spray", "railsched_lpt_spray_chunkwise", "railsched_eval",
                "railsched_schedule"):
+        getattr(lib, fn).restype = C.c_int
+    lib.railsched_route_logprobs.argtypes = [P, I32, I64, I32, I64, F32, P, P, I32, I32, P, P, P, P, P, P]
+    lib.railsched_route_logprobs_backward.argtypes = [P, I32, I64, I32, I64, F32, P, P, I32, P, P, P, I32, P, I64, P]
+    lib.railsched_route_balance_workspace_bytes.argtypes = [I64, I32, I32]
+    lib.railsched_route_balance_workspace_bytes.restype = SZ
+    lib.railsched_route_balance.argtypes = [P, I32, I64, I32, I64, P, P, I32, P, I32, F32, P, P, P, P, P, SZ, P]
+    lib.railsched_route_balance_backward.argtypes = [P, I32, I64, I32, I64, P, I32, P, I32, F32, P, P, P, I32, P, I64, P]
+    lib.railsched_route_distill.argtypes = [P, I32, I64, I32, I64, F32, P, P, P, P, I32, P, P]
+    lib.railsched_route_distill_backward.argtypes = [P, I32, I64, I32, I64, F32, P, P, P, P, I32, P, I32, P, I64, P]
+    for fn in ("railsched_route_logprobs", "railsched_route_logprobs_backward", "railsched_route_balance", "railsched_route_balance_backward",
+               "railsched_route_distill", "railsched_route_distill_backward"):
         getattr(lib, fn).restype = C.c_int
     _lib = lib
     return lib
@@ -491,3 +505,190 @@ def port_round_robin(chunk_off, rail, batch: int, topo: Topo, ports: int, capaci
     _check(load().railsched_port_round_robin(_ptr(chunk_off), _ptr(rail), batch, C.byref(t), ports, capacity, _ptr(port),
                                              _ptr(ws), ws.numel(), _stream()), "railsched_port_round_robin")
     return port
+
+
+# ---------------------------------------------------------------------------------- a router in training
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+class _Rows:
+    """Checks of the operators on a router's logits: tensors on one device, launches on that device's current stream."""
+
+    def __init__(self, logits: torch.Tensor):
+        if not logits.is_cuda:
+            raise ValueError("logits must be a device tensor")
+        if logits.dtype not in DTYPES:
+            raise ValueError(f"logits must be torch.float32, bfloat16 or float16, got {logits.dtype}")
+        self.device, self.dtype = logits.device, logits.dtype
+        self.rows, self.E, self.ld = self._strided(logits, "logits")
+        self.logits = logits
+
+    @staticmethod
+    def _strided(t: torch.Tensor, name: str):
+        if t.dim() != 2:
+            raise ValueError(f"{name} must have two dimensions")
+        rows, E = t.shape
+        if E > 1 and t.stride(1) != 1:
+            raise ValueError(f"the values of a row of {name} must be next to each other")
+        ld = t.stride(0) if rows > 1 else max(E, 1)
+        if ld < E:
+            raise ValueError(f"the rows of {name} must not overlap")
+        return rows, E, ld
+
+    @staticmethod
+    def width(t: Optional[torch.Tensor], name: str) -> int:
+        if t is None:
+            return 0
+        if t.dim() != 2:
+            raise ValueError(f"{name} must have two dimensions")
+        return t.shape[1]
+
+    def head(self):
+        return self.logits.data_ptr(), DTYPES[self.dtype], self.rows, self.E, self.ld
+
+    def arg(self, t: Optional[torch.Tensor], dtype, shape, name: str):
+        """The address of a contiguous tensor of this type and shape on the logits' device; None for None."""
+        if t is None:
+            return None
+        if t.device != self.device:
+            raise ValueError(f"{name} must be on {self.device}")
+        if t.dtype != dtype:
+            raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+        if t.shape != shape:
+            raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        return t.data_ptr()
+
+    def mask(self, t: Optional[torch.Tensor]):
+        if t is not None and t.dtype == torch.bool:
+            t = t.view(torch.uint8)
+        return self.arg(t, torch.uint8, (self.rows,), "row_mask")
+
+    def new(self, shape, dtype=torch.float32):
+        return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def gradient(self, out: Optional[torch.Tensor], accumulate: bool):
+        """(d_logits, its address, its row stride)"""
+        if out is None:
+            if accumulate:
+                raise ValueError("accumulate needs `out`, the gradient to add to")
+            out = self.new((self.rows, self.E), self.dtype)
+            return out, out.data_ptr(), max(self.E, 1)
+        if out.device != self.device or out.dtype != self.dtype or out.shape != (self.rows, self.E):
+            raise ValueError(f"out must be {self.dtype} of shape {(self.rows, self.E)} on {self.device}")
+        return out, out.data_ptr(), self._strided(out, "out")[2]
+
+    def call(self, name: str, *args):
+        """Runs an entry point on the current stream of the logits' device."""
+        fn = getattr(load(), name)
+        if torch.cuda.current_device() == self.device.index:
+            rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+        else:
+            with torch.cuda.device(self.device):
+                rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+        _check(rc, name)
+
+
+def route_logprobs(logits: torch.Tensor, topk_idx: Optional[torch.Tensor] = None, alternatives: int = 0, temperature: float = 1.0,
+                   row_mask: Optional[torch.Tensor] = None, out=None):
+    """Log probabilities of the experts topk_idx [rows][k], log-sum-exp and entropy of every row, and its `alternatives` most likely
+    experts: (logp or None, lse, entropy, alt_idx or None, alt_logp or None).  logits may be a view with a row stride.
+    out: a tuple of the same five, preallocated (lse and entropy may be None there: not computed)."""
+    r = _Rows(logits)
+    k, m = r.width(topk_idx, "topk_idx"), alternatives
+    if out is None:
+        out = (r.new((r.rows, k)) if k else None, r.new(r.rows), r.new(r.rows), r.new((r.rows, m), torch.int32) if m > 0 else None,
+               r.new((r.rows, m)) if m > 0 else None)
+    logp, lse, entropy, alt_idx, alt_logp = out
+    r.call("railsched_route_logprobs", *r.head(), temperature, r.mask(row_mask), r.arg(topk_idx, torch.int32, (r.rows, k), "topk_idx"), k, m,
+           r.arg(logp, torch.float32, (r.rows, k), "logp"), r.arg(lse, torch.float32, (r.rows,), "lse"),
+           r.arg(entropy, torch.float32, (r.rows,), "entropy"), r.arg(alt_idx, torch.int32, (r.rows, m), "alt_idx"),
+           r.arg(alt_logp, torch.float32, (r.rows, m), "alt_logp"))
+    return out
+
+
+def route_logprobs_backward(logits: torch.Tensor, topk_idx: Optional[torch.Tensor] = None, d_logp: Optional[torch.Tensor] = None,
+                            d_lse: Optional[torch.Tensor] = None, d_entropy: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                            row_mask: Optional[torch.Tensor] = None, accumulate: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient of the logits from those of logp, lse and entropy (None: 0).  accumulate: added to `out`."""
+    r = _Rows(logits)
+    k = r.width(topk_idx, "topk_idx")
+    out, to, ld_d = r.gradient(out, accumulate)
+    r.call("railsched_route_logprobs_backward", *r.head(), temperature, r.mask(row_mask), r.arg(topk_idx, torch.int32, (r.rows, k), "topk_idx"), k,
+           r.arg(d_logp, torch.float32, (r.rows, k), "d_logp"), r.arg(d_lse, torch.float32, (r.rows,), "d_lse"),
+           r.arg(d_entropy, torch.float32, (r.rows,), "d_entropy"), int(accumulate), to, ld_d)
+    return out
+
+
+def route_balance_workspace_bytes(rows: int, groups: int, E: int) -> int:
+    return int(load().railsched_route_balance_workspace_bytes(rows, groups, E))
+
+
+def _groups(r: _Rows, groups: int, group_off: Optional[torch.Tensor]):
+    if group_off is None:
+        return groups, None
+    if group_off.dim() != 1 or group_off.shape[0] < 1:
+        raise ValueError("group_off must hold groups + 1 offsets")
+    return group_off.shape[0] - 1, r.arg(group_off, torch.int64, group_off.shape, "group_off")
+
+
+def route_balance(logits: torch.Tensor, topk_idx: torch.Tensor, groups: int = 1, group_off: Optional[torch.Tensor] = None, coef: float = 1.0,
+                  row_mask: Optional[torch.Tensor] = None, out=None, ws: Optional[torch.Tensor] = None):
+    """Balance loss of groups of rows: (counts [groups][E] int64, tokens [groups] int64, prob_sum [groups][E], loss [groups]).
+    The groups are `groups` equal parts of the rows, or with group_off (int64 offsets) the rows between neighbouring offsets."""
+    r = _Rows(logits)
+    n, off = _groups(r, groups, group_off)
+    if out is None:
+        out = (r.new((n, r.E), torch.int64), r.new(n, torch.int64), r.new((n, r.E)), r.new(n))
+    counts, tokens, prob_sum, loss = out
+    k = r.width(topk_idx, "topk_idx")
+    if ws is None:
+        ws = _ws(route_balance_workspace_bytes(r.rows, n, r.E), r.device)
+    r.call("railsched_route_balance", *r.head(), r.mask(row_mask), r.arg(topk_idx, torch.int32, (r.rows, k), "topk_idx"), k, off, n, coef,
+           r.arg(counts, torch.int64, (n, r.E), "counts"), r.arg(tokens, torch.int64, (n,), "tokens"),
+           r.arg(prob_sum, torch.float32, (n, r.E), "prob_sum"), r.arg(loss, torch.float32, (n,), "loss"),
+           r.arg(ws, torch.uint8, ws.shape, "ws"), ws.numel())
+    return out
+
+
+def route_balance_backward(logits: torch.Tensor, k: int, counts: torch.Tensor, tokens: torch.Tensor, d_loss: torch.Tensor,
+                           group_off: Optional[torch.Tensor] = None, coef: float = 1.0, row_mask: Optional[torch.Tensor] = None,
+                           accumulate: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient of the logits from that of the losses, with the counts and tokens of route_balance (or their sums over ranks).
+    Rows of no group (before the first offset, behind the last one) are left as they are in `out`, and 0 without `out`."""
+    r = _Rows(logits)
+    n, off = _groups(r, counts.shape[0], group_off)
+    if out is None and off is not None and not accumulate:
+        out = torch.zeros((r.rows, r.E), dtype=r.dtype, device=r.device)
+    out, to, ld_d = r.gradient(out, accumulate)
+    r.call("railsched_route_balance_backward", *r.head(), r.mask(row_mask), k, off, n, coef, r.arg(counts, torch.int64, (n, r.E), "counts"),
+           r.arg(tokens, torch.int64, (n,), "tokens"), r.arg(d_loss, torch.float32, (n,), "d_loss"), int(accumulate), to, ld_d)
+    return out
+
+
+def route_distill(logits: torch.Tensor, teacher_idx: torch.Tensor, teacher_logits: torch.Tensor, teacher_lse: Optional[torch.Tensor] = None,
+                  temperature: float = 1.0, row_mask: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Divergence of every row's distribution from the teacher's list [rows][K] (and, with teacher_lse, the rest of the teacher's mass)."""
+    r = _Rows(logits)
+    K = r.width(teacher_idx, "teacher_idx")
+    if out is None:
+        out = r.new(r.rows)
+    r.call("railsched_route_distill", *r.head(), temperature, r.mask(row_mask), r.arg(teacher_idx, torch.int32, (r.rows, K), "teacher_idx"),
+           r.arg(teacher_logits, torch.float32, (r.rows, K), "teacher_logits"), r.arg(teacher_lse, torch.float32, (r.rows,), "teacher_lse"), K,
+           r.arg(out, torch.float32, (r.rows,), "out"))
+    return out
+
+
+def route_distill_backward(logits: torch.Tensor, teacher_idx: torch.Tensor, teacher_logits: torch.Tensor, d_loss: torch.Tensor,
+                           teacher_lse: Optional[torch.Tensor] = None, temperature: float = 1.0, row_mask: Optional[torch.Tensor] = None,
+                           accumulate: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient of the logits from that of route_distill's losses."""
+    r = _Rows(logits)
+    K = r.width(teacher_idx, "teacher_idx")
+    out, to, ld_d = r.gradient(out, accumulate)
+    r.call("railsched_route_distill_backward", *r.head(), temperature, r.mask(row_mask),
+           r.arg(teacher_idx, torch.int32, (r.rows, K), "teacher_idx"), r.arg(teacher_logits, torch.float32, (r.rows, K), "teacher_logits"),
+           r.arg(teacher_lse, torch.float32, (r.rows,), "teacher_lse"), K, r.arg(d_loss, torch.float32, (r.rows,), "d_loss"),
+           int(accumulate), to, ld_d)
+    return out

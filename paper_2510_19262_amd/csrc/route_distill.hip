@@ -1,0 +1,254 @@
+// Distillation of a router from the top logits of a teacher, and its gradient.
+//
+// Per row: the student's softmax from one read of its logits; the teacher's entries, one to a lane, their probabilities q, and the row in LDS
+// that marks the listed experts, so that the student's probability outside the list is a sum of its own terms (1 minus the listed ones would lose
+// it where the list holds nearly everything).
+//
+// The loss is formed as  sum_j (q log(q/p) - q + p) + rest + (sum of q and p outside these terms):  every term is >= 0 and of second order where
+// p is near q, so a student near its teacher keeps its loss to fp32's relative accuracy, where sum q (log q - log p) would be a difference of
+// larger terms.  With d = log p - log q:  q log(q/p) - q + p = q (e^d - 1 - d).
+#include "router_core.h"
+
+namespace rs {
+
+// e^d - 1 - d: a series near 0, where the difference cancels.  |d| < 1/2: d^2/2 (1 + d/3 (1 + d/4 (... (1 + d/10)))), next term below 2^-27 of it
+__device__ __forceinline__ float exp_above(float d)
+{
+    float s = 1.0f + d * (1.0f / 10);
+    s = 1.0f + d * (1.0f / 9) * s;
+    s = 1.0f + d * (1.0f / 8) * s;
+    s = 1.0f + d * (1.0f / 7) * s;
+    s = 1.0f + d * (1.0f / 6) * s;
+    s = 1.0f + d * (1.0f / 5) * s;
+    s = 1.0f + d * (1.0f / 4) * s;
+    s = 1.0f + d * (1.0f / 3) * s;
+    s *= 0.5f * d * d;
+    return fabsf(d) < 0.5f ? s : expf(d) - 1.0f - d;
+}
+// x - log(1 + x), x > -1, the same way: x^2 (1/2 - x/3 + x^2/4 - ...); |x| < 1/8: nine terms, next one below 2^-27
+__device__ __forceinline__ float above_log(float x)
+{
+    float s = 1.0f / 10;
+    s = 1.0f / 9 - x * s;
+    s = 1.0f / 8 - x * s;
+    s = 1.0f / 7 - x * s;
+    s = 1.0f / 6 - x * s;
+    s = 1.0f / 5 - x * s;
+    s = 1.0f / 4 - x * s;
+    s = 1.0f / 3 - x * s;
+    s = 1.0f / 2 - x * s;
+    return fabsf(x) < 0.125f ? s * x * x : x - log1pf(x);
+}
+
+// What both passes need of a row.
+template <int LANES, int VPL, int NK>
+struct Distilled {
+    float t[VPL], e[VPL];        // the student: z - top, e^(z - top)
+    RowSoft soft;
+    int at[NK];                  // this lane's entries: expert or -1
+    bool again[NK];              // an entry whose expert another entry of the list names too
+    float q[NK], p[NK];          // the teacher's and the student's probability
+    float d[NK];                 // log p - log q
+    float mass;                  // sum of q (1 without t_lse)
+    float gap;                   // sum of q - p over the entries (p of every expert once): with a tail p_r - q_r
+    float rest_q, rest_p;
+    bool listed;                 // whether the row has entries at all
+};
+
+template <typename T, int LANES, int VPL, bool VEC, int NK>
+__device__ __forceinline__ void distill_row(const T *__restrict__ logits, int64_t row, bool live, int E, int64_t ld, float inv_tau,
+                                            const int32_t *__restrict__ t_idx, const float *__restrict__ t_logit,
+                                            const float *__restrict__ t_lse, int K, int q0, float *mine, Distilled<LANES, VPL, NK> &o)
+{
+    const T *__restrict__ from = logits + row * ld;
+    row_values<T, LANES, VPL, VEC>(from, live, E, q0, o.t);
+    float tl[NK], xl[NK];
+    float best = -INFINITY;
+    bool any = false;
+#pragma unroll
+    for (int r = 0; r < NK; ++r) {
+        const int j = q0 + LANES * r;
+        const bool has = live && j < K;
+        o.at[r] = has ? t_idx[row * K + j] : -1;
+        tl[r] = has ? t_logit[row * K + j] : -INFINITY;
+        if (o.at[r] < 0 || o.at[r] >= E || tl[r] == -INFINITY) { o.at[r] = -1; tl[r] = -INFINITY; }
+        xl[r] = o.at[r] >= 0 ? (float)from[o.at[r]] : 0.0f;
+        best = fmaxf(best, tl[r]);
+        any |= o.at[r] >= 0;
+    }
+    o.listed = row_any<LANES>(any);
+    lds_fill<LANES, VPL, VEC>(mine, q0, -1.0f);
+    lds_order();
+    lds_mark<LANES, NK>(mine, q0, o.at, o.again);
+    o.soft = row_softmax<LANES, VPL>(o.t, o.e, inv_tau);
+    const float log_total = logf(o.soft.total), scale = 1.0f / o.soft.total;
+    best = row_max<LANES>(best);
+    // log of the teacher's total mass, in the same units as z
+    float log_mass;
+    if (t_lse) {
+        log_mass = live ? t_lse[row] : 0.0f;
+    } else {
+        float s = 0.0f;
+#pragma unroll
+        for (int r = 0; r < NK; ++r) s += o.at[r] >= 0 ? expf((tl[r] - best) * inv_tau) : 0.0f;
+        log_mass = best * inv_tau + logf(row_sum<LANES>(s));
+    }
+    const float shift = (log_mass - o.soft.top) - log_total;
+    float mass = 0.0f, gap = 0.0f;
+#pragma unroll
+    for (int r = 0; r < NK; ++r) {
+        const bool has = o.at[r] >= 0;
+        o.q[r] = has ? expf(tl[r] * inv_tau - log_mass) : 0.0f;
+        o.p[r] = has ? exp_of(xl[r] * inv_tau - o.soft.top) * scale : 0.0f;
+        o.d[r] = (xl[r] - tl[r]) * inv_tau + shift;
+        mass += o.q[r];
+        gap += o.q[r] - (o.again[r] ? 0.0f : o.p[r]);
+    }
+    o.mass = t_lse ? row_sum<LANES>(mass) : 1.0f;
+    o.gap = row_sum<LANES>(gap);
+    float marks[VPL], outside = 0.0f;
+    lds_values<LANES, VPL, VEC>(mine, q0, marks);
+#pragma unroll
+    for (int j = 0; j < VPL; ++j) outside += marks[j] < 0.0f ? o.e[j] : 0.0f;
+    o.rest_p = row_sum<LANES>(outside) * scale;
+    o.rest_q = t_lse && o.rest_p > 0.0f ? fmaxf(1.0f - o.mass, 0.0f) : 0.0f;
+}
+
+template <typename T, int LANES, int VPL, bool VEC, int NK>
+__global__ __launch_bounds__(256) void route_distill_kernel(const T *__restrict__ logits, int64_t rows, int E, int64_t ld, float tau,
+                                                            const uint8_t *__restrict__ row_mask, const int32_t *__restrict__ t_idx,
+                                                            const float *__restrict__ t_logit, const float *__restrict__ t_lse, int K,
+                                                            float *__restrict__ loss)
+{
+    constexpr int ROWS_PER_BLOCK = 256 / LANES;
+    __shared__ __align__(16) float lds[ROWS_PER_BLOCK * LANES * VPL];
+    const int q0 = threadIdx.x % LANES;
+    float *mine = lds + threadIdx.x / LANES * (LANES * VPL);
+    const float inv_tau = 1.0f / tau;
+    const int64_t stride = (int64_t)gridDim.x * ROWS_PER_BLOCK;
+    for (int64_t w0 = (int64_t)blockIdx.x * ROWS_PER_BLOCK; w0 < rows; w0 += stride) {
+        const int64_t row = w0 + threadIdx.x / LANES;
+        const bool there = row < rows;
+        const bool live = there && (!row_mask || row_mask[row] != 0);
+        Distilled<LANES, VPL, NK> o;
+        distill_row<T, LANES, VPL, VEC, NK>(logits, row, live, E, ld, inv_tau, t_idx, t_logit, t_lse, K, q0, mine, o);
+        float terms = 0.0f, twice = 0.0f;
+#pragma unroll
+        for (int r = 0; r < NK; ++r) {
+            if (o.at[r] >= 0) {
+                // q (e^d - 1 - d) where e^d does not carry it off, and p alone where q has vanished
+                terms += o.q[r] == 0.0f ? o.p[r] : o.d[r] < 1.0f ? o.q[r] * exp_above(o.d[r]) : o.p[r] - o.q[r] - o.q[r] * o.d[r];
+                if (o.again[r]) twice += o.p[r];
+            }
+        }
+        terms = row_sum<LANES>(terms);
+        twice = row_sum<LANES>(twice);
+        // sum q + q_r - (sum of p over the entries and outside): p of an expert listed twice is in its terms twice
+        float sum = terms - twice;
+        if (o.rest_q > 0.0f) {
+            const float apart = o.gap / o.rest_q;                        // p_r / q_r - 1
+            sum += o.rest_q * above_log(apart);
+        } else {
+            sum += o.rest_p + (o.mass - 1.0f);
+        }
+        if (there && q0 == 0) loss[row] = o.soft.total != 0.0f && o.listed ? tau * tau * sum : 0.0f;
+        lds_order();
+    }
+}
+
+template <typename T, int LANES, int VPL, bool VEC, int NK>
+__global__ __launch_bounds__(256) void route_distill_backward_kernel(const T *__restrict__ logits, int64_t rows, int E, int64_t ld, float tau,
+                                                                     const uint8_t *__restrict__ row_mask, const int32_t *__restrict__ t_idx,
+                                                                     const float *__restrict__ t_logit, const float *__restrict__ t_lse, int K,
+                                                                     const float *__restrict__ d_loss, int add, T *__restrict__ d_logits,
+                                                                     int64_t ld_d)
+{
+    constexpr int ROWS_PER_BLOCK = 256 / LANES;
+    __shared__ __align__(16) float lds[ROWS_PER_BLOCK * LANES * VPL];
+    const int q0 = threadIdx.x % LANES;
+    float *mine = lds + threadIdx.x / LANES * (LANES * VPL);
+    const float inv_tau = 1.0f / tau;
+    const int64_t stride = (int64_t)gridDim.x * ROWS_PER_BLOCK;
+    for (int64_t w0 = (int64_t)blockIdx.x * ROWS_PER_BLOCK; w0 < rows; w0 += stride) {
+        const int64_t row = w0 + threadIdx.x / LANES;
+        const bool there = row < rows;
+        const bool live = there && (!row_mask || row_mask[row] != 0);
+        Distilled<LANES, VPL, NK> o;
+        distill_row<T, LANES, VPL, VEC, NK>(logits, row, live, E, ld, inv_tau, t_idx, t_logit, t_lse, K, q0, mine, o);
+        const bool counts = o.soft.total != 0.0f;
+        lds_order();
+        lds_put<LANES, NK>(mine, q0, o.at, o.again, o.q);
+        float listed[VPL];
+        lds_values<LANES, VPL, VEC>(mine, q0, listed);
+        lds_order();
+        const float unit = live && o.listed ? tau * d_loss[row] : 0.0f;
+        const float scale = 1.0f / o.soft.total;
+        const float inside = (o.mass + o.rest_q) * scale;
+        // Q + q_r - q_r / p_r is (p_r - q_r) / p_r where sum q + q_r is 1
+        const float outside = (o.rest_q > 0.0f ? o.gap / o.rest_p : o.mass) * scale;
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) {
+            const float g = listed[j] < 0.0f ? o.e[j] * outside : o.e[j] * inside - listed[j];
+            o.t[j] = counts && o.listed ? unit * g : 0.0f;
+        }
+        if (there && (counts || !add)) row_store<T, LANES, VPL, VEC>(d_logits + row * ld_d, E, q0, add != 0, o.t);
+    }
+}
+
+template <typename F>
+static int launch_distill(int64_t rows, int lanes, F launch)
+{
+    const int64_t blocks = (rows + 256 / lanes - 1) / (256 / lanes);
+    launch(dim3((unsigned)(blocks < (1 << 22) ? blocks : 1 << 22)));
+    return launch_status();
+}
+
+static int check_distill(int64_t rows, int32_t E, const int32_t *t_idx, const float *t_logit, int32_t K)
+{
+    if (K < 1 || K > E) return RAILSCHED_ERR_INVALID_ARG;
+    if (K > kMaxListed) return RAILSCHED_ERR_UNSUPPORTED;
+    if (rows > 0 && (!t_idx || !t_logit)) return RAILSCHED_ERR_NULL_PTR;
+    return RAILSCHED_OK;
+}
+
+}  // namespace rs
+
+extern "C" int railsched_route_distill(const void *logits, int32_t dtype, int64_t rows, int32_t E, int64_t ld, float temperature,
+                                       const uint8_t *row_mask, const int32_t *t_idx, const float *t_logit, const float *t_lse, int32_t K,
+                                       float *loss, void *stream)
+{
+    using namespace rs;
+    if (int rc = check_router(logits, dtype, rows, E, ld, temperature)) return rc;
+    if (int rc = check_distill(rows, E, t_idx, t_logit, K)) return rc;
+    if (rows == 0) return RAILSCHED_OK;
+    if (!loss) return RAILSCHED_ERR_NULL_PTR;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return by_dtype(dtype, [&](auto t) {
+        using T = decltype(t);
+        return launch_distill(rows, 64, [&](dim3 grid) {
+            hipLaunchKernelGGL((route_distill_kernel<T, 64, 16, false, 1>), grid, dim3(256), 0, st, static_cast<const T *>(logits), rows, E, ld, temperature,
+                               row_mask, t_idx, t_logit, t_lse, K, loss);
+        });
+    });
+}
+
+extern "C" int railsched_route_distill_backward(const void *logits, int32_t dtype, int64_t rows, int32_t E, int64_t ld, float temperature,
+                                                const uint8_t *row_mask, const int32_t *t_idx, const float *t_logit, const float *t_lse,
+                                                int32_t K, const float *d_loss, int32_t accumulate, void *d_logits, int64_t ld_d,
+                                                void *stream)
+{
+    using namespace rs;
+    if (int rc = check_router(logits, dtype, rows, E, ld, temperature)) return rc;
+    if (int rc = check_gradient(logits, d_logits, rows, E, ld_d, accumulate)) return rc;
+    if (int rc = check_distill(rows, E, t_idx, t_logit, K)) return rc;
+    if (rows == 0) return RAILSCHED_OK;
+    if (!d_loss) return RAILSCHED_ERR_NULL_PTR;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return by_dtype(dtype, [&](auto t) {
+        using T = decltype(t);
+        return launch_distill(rows, 64, [&](dim3 grid) {
+            hipLaunchKernelGGL((route_distill_backward_kernel<T, 64, 16, false, 1>), grid, dim3(256), 0, st, static_cast<const T *>(logits), rows, E, ld,
+                               temperature, row_mask, t_idx, t_logit, t_lse, K, d_loss, accumulate, static_cast<T *>(d_logits), ld_d);
+        });
+    });
+}

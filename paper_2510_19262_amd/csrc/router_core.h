@@ -1,0 +1,266 @@
+// Device-side pieces of the operators on a router's logits (log probabilities, balance loss, distillation): rows of
+// E <= 1024 logits held in registers by LANES consecutive lanes, VPL values each, their softmax, and a row in LDS
+// through which values listed by expert (picks, a teacher's entries) reach the lanes that hold the experts.
+#pragma once
+
+#include "topk_core.h"
+
+namespace rs {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16_t;
+typedef _Float16 f16_t;
+
+constexpr int kMaxListed = 64;     // alternatives of a row, entries of a teacher's list
+
+// ---- four consecutive values: 16 bytes of fp32, 8 of the short types; streaming, as every logit is read once
+template <typename T>
+__device__ __forceinline__ void load4(const T *p, float (&v)[4])
+{
+    if constexpr (sizeof(T) == 4) {
+        const f32x4 x = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p));
+        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+    } else {
+        const u16x4 x = __builtin_bit_cast(u16x4, __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(p)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (float)__builtin_bit_cast(T, (uint16_t)x[i]);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store4(T *p, const float (&v)[4])
+{
+    if constexpr (sizeof(T) == 4) {
+        f32x4 x;
+        x.x = v[0]; x.y = v[1]; x.z = v[2]; x.w = v[3];
+        __builtin_nontemporal_store(x, reinterpret_cast<f32x4 *>(p));
+    } else {
+        u16x4 x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __builtin_bit_cast(uint16_t, (T)v[i]);      // to nearest, ties to even
+        __builtin_nontemporal_store(__builtin_bit_cast(u32x2, x), reinterpret_cast<u32x2 *>(p));
+    }
+}
+
+// ---- sums and maxima over the LANES lanes of a row, in all of them
+template <int LANES, typename F>
+__device__ __forceinline__ float row_reduce(float v, F op)
+{
+    if constexpr (LANES >= 2) v = op(v, xlane<1>(v));
+    if constexpr (LANES >= 4) v = op(v, xlane<2>(v));
+    if constexpr (LANES >= 8) v = op(v, xlane<4>(v));
+    if constexpr (LANES >= 16) v = op(v, xlane<8>(v));
+    if constexpr (LANES >= 32) v = op(v, xlane<16>(v));
+    if constexpr (LANES >= 64) v = op(v, xlane<32>(v));
+    return v;
+}
+template <int LANES>
+__device__ __forceinline__ float row_max(float v) { return row_reduce<LANES>(v, [](float a, float b) { return fmaxf(a, b); }); }
+template <int LANES>
+__device__ __forceinline__ float row_sum(float v) { return row_reduce<LANES>(v, [](float a, float b) { return a + b; }); }
+
+// whether any lane of this lane's row says so
+template <int LANES>
+__device__ __forceinline__ bool row_any(bool v)
+{
+    const unsigned long long all = __ballot(v);
+    if constexpr (LANES == 64) return all != 0ull;
+    else return ((all >> (threadIdx.x & 63u & ~(unsigned)(LANES - 1))) & ((1ull << LANES) - 1ull)) != 0ull;
+}
+
+// This lane's values of a row as fp32; places that do not exist (and whole rows that are not live, which are not read) are -infinity.
+// VEC: places of four consecutive experts, interleaved over the lanes, as slot_index() numbers them.
+template <typename T, int LANES, int VPL, bool VEC>
+__device__ __forceinline__ void row_values(const T *__restrict__ row, bool live, int E, int q, float (&x)[VPL])
+{
+    if constexpr (VEC) {
+#pragma unroll
+        for (int c = 0; c < VPL / 4; ++c) {
+            float v[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            const int e0 = 4 * (q + LANES * c);
+            if (live && e0 < E) load4(row + e0, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[4 * c + i] = v[i];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) {
+            const int e = q + LANES * j;
+            x[j] = (live && e < E) ? (float)row[e] : -INFINITY;
+        }
+    }
+}
+
+// The gradient of a row: written, or added to what is there.
+template <typename T, int LANES, int VPL, bool VEC>
+__device__ __forceinline__ void row_store(T *__restrict__ row, int E, int q, bool add, const float (&x)[VPL])
+{
+    if constexpr (VEC) {
+#pragma unroll
+        for (int c = 0; c < VPL / 4; ++c) {
+            const int e0 = 4 * (q + LANES * c);
+            if (e0 < E) {
+                float v[4];
+                if (add) load4(row + e0, v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = add ? v[i] + x[4 * c + i] : x[4 * c + i];
+                store4(row + e0, v);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) {
+            const int e = q + LANES * j;
+            if (e < E) row[e] = (T)(add ? (float)row[e] + x[j] : x[j]);
+        }
+    }
+}
+
+// exp(t) by the hardware's power of two: t <= 0, so the rounding of t * log2(e) is at most |t| 2^-24 of a value e^t, below 2^-25 of the
+// row's largest
+__device__ __forceinline__ float exp_of(float t) { return __builtin_amdgcn_exp2f(t * 1.44269504088896341f); }
+
+// Softmax of a row: x holds the logits on entry and t = z - max z on return, e the exponentials of t.
+struct RowSoft {
+    float top;      // the largest z (0 in a row without one)
+    float total;    // sum of e: at least 1, or 0 in a row that does not count (every logit -infinity), or NaN
+};
+template <int LANES, int VPL>
+__device__ __forceinline__ RowSoft row_softmax(float (&x)[VPL], float (&e)[VPL], float inv_tau)
+{
+    RowSoft r;
+    float m = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < VPL; ++j) {
+        x[j] *= inv_tau;
+        m = fmaxf(m, x[j]);
+    }
+    m = row_max<LANES>(m);
+    r.top = m == -INFINITY ? 0.0f : m;
+    float s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < VPL; ++j) {
+        x[j] -= r.top;
+        e[j] = exp_of(x[j]);
+        s += e[j];
+    }
+    r.total = row_sum<LANES>(s);
+    return r;
+}
+
+// sum of e t over the row (e 0 where t is -infinity: the product is 0 there)
+template <int LANES, int VPL>
+__device__ __forceinline__ float row_dot_t(const float (&t)[VPL], const float (&e)[VPL])
+{
+    float a = 0.0f;
+#pragma unroll
+    for (int j = 0; j < VPL; ++j) a += e[j] * fmaxf(t[j], -1e30f);
+    return row_sum<LANES>(a);
+}
+
+// ---- a row of LANES * VPL floats in LDS for every row of the wavefront.  Only lanes of one wavefront meet in it, and a wavefront's LDS
+// accesses are carried out in order: a fence that keeps the compiler from moving them is all that is needed.
+__device__ __forceinline__ void lds_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+template <int LANES, int VPL, bool VEC>
+__device__ __forceinline__ void lds_fill(float *row, int q, float value)
+{
+#pragma unroll
+    for (int c = 0; c < VPL / 4; ++c) {                  // every place belongs to one lane, whatever the order
+        f32x4 v;
+        v.x = v.y = v.z = v.w = value;
+        *reinterpret_cast<f32x4 *>(row + 4 * (q + LANES * c)) = v;
+    }
+}
+template <int LANES, int VPL, bool VEC>
+__device__ __forceinline__ void lds_values(const float *row, int q, float (&x)[VPL])
+{
+    if constexpr (VEC) {
+#pragma unroll
+        for (int c = 0; c < VPL / 4; ++c) {
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(row + 4 * (q + LANES * c));
+            x[4 * c + 0] = v.x; x[4 * c + 1] = v.y; x[4 * c + 2] = v.z; x[4 * c + 3] = v.w;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) x[j] = row[q + LANES * j];
+    }
+}
+
+// Marks the places at[r] (-1: none) of this lane's entries q, q + LANES, ... in the row; on return again[r] says that another entry of the same
+// place holds it (of several entries with one place exactly one is not `again`).  The marked places hold values >= 0.
+template <int LANES, int N>
+__device__ __forceinline__ void lds_mark(float *row, int q, const int (&at)[N], bool (&again)[N])
+{
+#pragma unroll
+    for (int r = 0; r < N; ++r)
+        if (at[r] >= 0) row[at[r]] = (float)(q + LANES * r);
+    lds_order();
+#pragma unroll
+    for (int r = 0; r < N; ++r) again[r] = at[r] >= 0 && row[at[r]] != (float)(q + LANES * r);
+    lds_order();
+}
+
+// Puts value[r] at the marked places; entries of one place are added up in the order of the entries, so that equal inputs give equal bits.
+template <int LANES, int N>
+__device__ __forceinline__ void lds_put(float *row, int q, const int (&at)[N], const bool (&again)[N], const float (&value)[N])
+{
+    bool any = false;
+#pragma unroll
+    for (int r = 0; r < N; ++r) any |= again[r];
+    if (__ballot(any) == 0ull) {
+#pragma unroll
+        for (int r = 0; r < N; ++r)
+            if (at[r] >= 0) row[at[r]] = value[r];
+    } else {                                             // an expert listed twice: one entry after the other
+#pragma unroll
+        for (int r = 0; r < N; ++r)
+            if (at[r] >= 0) row[at[r]] = 0.0f;
+        lds_order();
+#pragma unroll
+        for (int r = 0; r < N; ++r)
+            for (int i = 0; i < LANES; ++i) {
+                if (q == i && at[r] >= 0) row[at[r]] += value[r];
+                lds_order();
+            }
+    }
+    lds_order();
+}
+
+// ---- host side
+inline int check_router(const void *logits, int32_t dtype, int64_t rows, int32_t E, int64_t ld, float temperature)
+{
+    if (dtype < RAILSCHED_F32 || dtype > RAILSCHED_F16 || rows < 0 || E < 1 || ld < E) return RAILSCHED_ERR_INVALID_ARG;
+    if (!(temperature > 0.0f) || !(temperature <= 3.402823466e38f)) return RAILSCHED_ERR_INVALID_ARG;
+    if (E > kMaxExperts || rows > 0x7FFFFFFFll || ld > (int64_t(1) << 31)) return RAILSCHED_ERR_UNSUPPORTED;
+    if (rows > 0 && !logits) return RAILSCHED_ERR_NULL_PTR;
+    return RAILSCHED_OK;
+}
+inline int check_gradient(const void *logits, const void *d_logits, int64_t rows, int32_t E, int64_t ld_d, int32_t accumulate)
+{
+    if (ld_d < E || (accumulate != 0 && accumulate != 1)) return RAILSCHED_ERR_INVALID_ARG;
+    if (ld_d > (int64_t(1) << 31)) return RAILSCHED_ERR_UNSUPPORTED;
+    if (rows > 0 && !d_logits) return RAILSCHED_ERR_NULL_PTR;
+    if (rows > 0 && d_logits == logits) return RAILSCHED_ERR_INVALID_ARG;
+    return RAILSCHED_OK;
+}
+// whether rows can be read or written four values at a time
+template <typename T>
+inline bool in_fours(const void *p, int32_t E, int64_t ld)
+{
+    return E % 4 == 0 && ld % 4 == 0 && reinterpret_cast<uintptr_t>(p) % (4 * sizeof(T)) == 0;
+}
+
+// f(T()) for the type that dtype names
+template <typename F>
+inline int by_dtype(int32_t dtype, F f)
+{
+    if (dtype == RAILSCHED_BF16) return f(bf16_t());
+    if (dtype == RAILSCHED_F16) return f(f16_t());
+    return f(float());
+}
+
+}  // namespace rs
