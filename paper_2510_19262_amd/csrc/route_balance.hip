@@ -131,6 +131,8 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
                                                                      int add, T *__restrict__ d_logits, int64_t ld_d)
 {
     constexpr int ROWS_PER_BLOCK = 256 / LANES;
+    __shared__ double part[256];
+    __shared__ float weight[kMaxExperts];
     const int q = threadIdx.x % LANES, slot = threadIdx.x / LANES;
     const int64_t r0 = blockIdx.x * slice_rows;
     const int64_t r1 = r0 + slice_rows < groups.rows ? r0 + slice_rows : groups.rows;
@@ -139,16 +141,25 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
         if (gb >= r1) break;
         const int64_t lo = gb > r0 ? gb : r0, hi = ge < r1 ? ge : r1;
         if (lo >= hi) continue;
-        double mean = 0.0;
-        for (int i = 0; i < E; ++i) mean += (double)counts[(int64_t)g * E + i];
-        mean /= E;
-        const double n = (double)tokens[g];
+        const int64_t *__restrict__ c = counts + (int64_t)g * E;
+        double sum = 0.0;
+        for (int i = threadIdx.x; i < E; i += 256) sum += (double)c[i];
+        part[threadIdx.x] = sum;
+        __syncthreads();
+#pragma unroll
+        for (int w = 128; w >= 1; w /= 2) {
+            if (threadIdx.x < w) part[threadIdx.x] += part[threadIdx.x + w];
+            __syncthreads();
+        }
+        const double mean = part[0] / E, n = (double)tokens[g];
         const double unit = n > 0.0 ? (double)d_loss[g] * coef * E / ((double)k * n * n) : 0.0;
+        for (int i = threadIdx.x; i < E; i += 256) weight[i] = (float)(unit * ((double)c[i] - mean));
+        __syncthreads();
         float a[VPL];
 #pragma unroll
         for (int j = 0; j < VPL; ++j) {
             const int i = slot_index<LANES, VPL, VEC>(q, j);
-            a[j] = i < E ? (float)(unit * ((double)counts[(int64_t)g * E + i] - mean)) : 0.0f;
+            a[j] = i < E ? weight[i] : 0.0f;
         }
         for (int64_t w0 = lo; w0 < hi; w0 += ROWS_PER_BLOCK) {
             const int64_t row = w0 + slot;
@@ -170,16 +181,18 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
             for (int j = 0; j < VPL; ++j) t[j] = counts_here ? e[j] * (a[j] - ap) : 0.0f;
             if (there && (counts_here || !add)) row_store<T, LANES, VPL, VEC>(d_logits + row * ld_d, E, q, add != 0, t);
         }
+        __syncthreads();
     }
 }
 
-// rows of a slice: 2048 slices fill the GPU eight workgroups to a CU; no fewer than 64 rows, so that the records stay few against the logits
-static int64_t balance_slice_rows(int64_t rows)
+// rows of a slice: 2048 slices fill the GPU eight workgroups to a CU; no fewer than the rows that a workgroup has in hand at once, nor than 64, so that
+// the records stay few against the logits
+static int64_t balance_slice_rows(int64_t rows, int E)
 {
-    const int64_t r = (rows + 2047) / 2048;
-    return r > 64 ? r : 64;
+    const int64_t r = (rows + 2047) / 2048, least = E <= 8 ? 128 : 64;
+    return r > least ? r : least;
 }
-static int64_t balance_slices(int64_t rows) { return (rows + balance_slice_rows(rows) - 1) / balance_slice_rows(rows); }
+static int64_t balance_slices(int64_t rows, int E) { return (rows + balance_slice_rows(rows, E) - 1) / balance_slice_rows(rows, E); }
 
 static int check_groups(int64_t rows, const int64_t *group_off, int32_t groups)
 {
@@ -202,7 +215,7 @@ extern "C" size_t railsched_route_balance_workspace_bytes(int64_t rows, int32_t 
 {
     using namespace rs;
     if (rows < 0 || rows > 0x7FFFFFFFll || groups < 0 || E < 1 || E > kMaxExperts) return 0;
-    return align_up((size_t)(balance_slices(rows) + groups + 1) * Record::words(E) * sizeof(float), 256);
+    return align_up((size_t)(balance_slices(rows, E) + groups + 1) * Record::words(E) * sizeof(float), 256);
 }
 
 extern "C" int railsched_route_balance(const void *logits, int32_t dtype, int64_t rows, int32_t E, int64_t ld, const uint8_t *row_mask,
@@ -219,14 +232,17 @@ extern "C" int railsched_route_balance(const void *logits, int32_t dtype, int64_
     if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 != 0 || ws_bytes < railsched_route_balance_workspace_bytes(rows, groups, E)) return RAILSCHED_ERR_WORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const Groups gr = make_groups(rows, group_off, groups);
-    const int64_t slice_rows = balance_slice_rows(rows);
+    const int64_t slice_rows = balance_slice_rows(rows, E);
     float *records = static_cast<float *>(ws);
     if (rows > 0) {
         const int rc = by_dtype(dtype, [&](auto t) {
             using T = decltype(t);
-            hipLaunchKernelGGL((route_balance_kernel<T, 64, 16, false>), dim3((unsigned)balance_slices(rows)), dim3(256), 0, st,
-                               static_cast<const T *>(logits), E, ld, row_mask, topk_idx, k, gr, slice_rows, records);
-            return launch_status();
+            return by_shape(E, in_fours<T>(logits, E, ld), [&](auto s) {
+                using S = decltype(s);
+                hipLaunchKernelGGL((route_balance_kernel<T, S::LANES, S::VPL, S::VEC>), dim3((unsigned)balance_slices(rows, E)), dim3(256), 0, st,
+                                   static_cast<const T *>(logits), E, ld, row_mask, topk_idx, k, gr, slice_rows, records);
+                return launch_status();
+            });
         });
         if (rc) return rc;
     }
@@ -251,9 +267,12 @@ extern "C" int railsched_route_balance_backward(const void *logits, int32_t dtyp
     const Groups gr = make_groups(rows, group_off, groups);
     return by_dtype(dtype, [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL((route_balance_backward_kernel<T, 64, 16, false>), dim3((unsigned)balance_slices(rows)), dim3(256), 0, st,
-                           static_cast<const T *>(logits), E, ld, row_mask, k, gr, balance_slice_rows(rows), coef, counts, tokens, d_loss, accumulate,
-                           static_cast<T *>(d_logits), ld_d);
-        return launch_status();
+        return by_shape(E, in_fours<T>(logits, E, ld) && in_fours<T>(d_logits, E, ld_d), [&](auto s) {
+            using S = decltype(s);
+            hipLaunchKernelGGL((route_balance_backward_kernel<T, S::LANES, S::VPL, S::VEC>), dim3((unsigned)balance_slices(rows, E)), dim3(256), 0, st,
+                               static_cast<const T *>(logits), E, ld, row_mask, k, gr, balance_slice_rows(rows, E), coef, counts, tokens, d_loss,
+                               accumulate, static_cast<T *>(d_logits), ld_d);
+            return launch_status();
+        });
     });
 }

@@ -225,9 +225,12 @@ extern "C" int railsched_route_distill(const void *logits, int32_t dtype, int64_
     hipStream_t st = static_cast<hipStream_t>(stream);
     return by_dtype(dtype, [&](auto t) {
         using T = decltype(t);
-        return launch_distill(rows, 64, [&](dim3 grid) {
-            hipLaunchKernelGGL((route_distill_kernel<T, 64, 16, false, 1>), grid, dim3(256), 0, st, static_cast<const T *>(logits), rows, E, ld, temperature,
-                               row_mask, t_idx, t_logit, t_lse, K, loss);
+        return by_shape(E, in_fours<T>(logits, E, ld), [&](auto s) {
+            using S = decltype(s);
+            return launch_distill(rows, S::LANES, [&](dim3 grid) {
+                hipLaunchKernelGGL((route_distill_kernel<T, S::LANES, S::VPL, S::VEC, list_regs<S>()>), grid, dim3(256), 0, st,
+                                   static_cast<const T *>(logits), rows, E, ld, temperature, row_mask, t_idx, t_logit, t_lse, K, loss);
+            });
         });
     });
 }
@@ -246,9 +249,13 @@ extern "C" int railsched_route_distill_backward(const void *logits, int32_t dtyp
     hipStream_t st = static_cast<hipStream_t>(stream);
     return by_dtype(dtype, [&](auto t) {
         using T = decltype(t);
-        return launch_distill(rows, 64, [&](dim3 grid) {
-            hipLaunchKernelGGL((route_distill_backward_kernel<T, 64, 16, false, 1>), grid, dim3(256), 0, st, static_cast<const T *>(logits), rows, E, ld,
-                               temperature, row_mask, t_idx, t_logit, t_lse, K, d_loss, accumulate, static_cast<T *>(d_logits), ld_d);
+        return by_shape(E, in_fours<T>(logits, E, ld) && in_fours<T>(d_logits, E, ld_d), [&](auto s) {
+            using S = decltype(s);
+            return launch_distill(rows, S::LANES, [&](dim3 grid) {
+                hipLaunchKernelGGL((route_distill_backward_kernel<T, S::LANES, S::VPL, S::VEC, list_regs<S>()>), grid, dim3(256), 0, st,
+                                   static_cast<const T *>(logits), rows, E, ld, temperature, row_mask, t_idx, t_logit, t_lse, K, d_loss, accumulate,
+                                   static_cast<T *>(d_logits), ld_d);
+            });
         });
     });
 }

@@ -162,8 +162,11 @@ extern "C" int railsched_route_logprobs(const void *logits, int32_t dtype, int64
     hipStream_t st = static_cast<hipStream_t>(stream);
     return by_dtype(dtype, [&](auto t) {
         using T = decltype(t);
-        return launch_logprobs<T, 64, 16, false>(static_cast<const T *>(logits), rows, st, E, ld, 1.0f / temperature, row_mask, topk_idx, k, m, logp,
-                                                 lse, entropy, alt_idx, alt_logp);
+        return by_shape(E, in_fours<T>(logits, E, ld), [&](auto s) {
+            using S = decltype(s);
+            return launch_logprobs<T, S::LANES, S::VPL, S::VEC>(static_cast<const T *>(logits), rows, st, E, ld, 1.0f / temperature, row_mask, topk_idx, k,
+                                                                m, logp, lse, entropy, alt_idx, alt_logp);
+        });
     });
 }
 
@@ -181,7 +184,11 @@ extern "C" int railsched_route_logprobs_backward(const void *logits, int32_t dty
     hipStream_t st = static_cast<hipStream_t>(stream);
     return by_dtype(dtype, [&](auto t) {
         using T = decltype(t);
-        return launch_logprobs_backward<T, 64, 16, false, 1>(static_cast<const T *>(logits), rows, st, E, ld, 1.0f / temperature, row_mask, topk_idx,
-                                                             k, k > 0 ? d_logp : nullptr, d_lse, d_entropy, accumulate, static_cast<T *>(d_logits), ld_d);
+        return by_shape(E, in_fours<T>(logits, E, ld) && in_fours<T>(d_logits, E, ld_d), [&](auto s) {
+            using S = decltype(s);
+            return launch_logprobs_backward<T, S::LANES, S::VPL, S::VEC, 1>(static_cast<const T *>(logits), rows, st, E, ld, 1.0f / temperature, row_mask,
+                                                                            topk_idx, k, k > 0 ? d_logp : nullptr, d_lse, d_entropy, accumulate,
+                                                                            static_cast<T *>(d_logits), ld_d);
+        });
     });
 }

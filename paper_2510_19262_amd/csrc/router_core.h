@@ -254,6 +254,36 @@ inline bool in_fours(const void *p, int32_t E, int64_t ld)
     return E % 4 == 0 && ld % 4 == 0 && reinterpret_cast<uintptr_t>(p) % (4 * sizeof(T)) == 0;
 }
 
+// The shape a row of E logits is held in: LANES lanes, VPL values each, in places of four or one by one.
+template <int L, int V, bool F>
+struct Shape {
+    static constexpr int LANES = L, VPL = V;
+    static constexpr bool VEC = F;
+};
+// f(Shape) for rows of E logits.  The fewest lanes that leave at most 16 values to each (more would cost occupancy): every lane less is a step less in the
+// row's sums and more rows to a wavefront.  Rows that are read one by one have fewer shapes, as they are rare.
+template <typename F>
+inline int by_shape(int E, bool fours, F f)
+{
+    if (!fours) {
+        if (E <= 16) return f(Shape<4, 4, false>());
+        if (E <= 64) return f(Shape<8, 8, false>());
+        if (E <= 256) return f(Shape<16, 16, false>());
+        return f(Shape<64, 16, false>());
+    }
+    if (E <= 8) return f(Shape<2, 4, true>());
+    if (E <= 16) return f(Shape<4, 4, true>());
+    if (E <= 32) return f(Shape<8, 4, true>());
+    if (E <= 64) return f(Shape<8, 8, true>());
+    if (E <= 128) return f(Shape<8, 16, true>());
+    if (E <= 256) return f(Shape<16, 16, true>());
+    if (E <= 512) return f(Shape<32, 16, true>());
+    return f(Shape<64, 16, true>());
+}
+// lists of at most kMaxListed entries, and of at most E, over the lanes of a row
+template <typename S>
+constexpr int list_regs() { return S::VPL < kMaxListed / S::LANES ? S::VPL : kMaxListed / S::LANES; }
+
 // f(T()) for the type that dtype names
 template <typename F>
 inline int by_dtype(int32_t dtype, F f)
