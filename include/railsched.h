@@ -307,13 +307,13 @@ int railsched_port_round_robin(const int64_t *chunk_off, const uint8_t *rail, in
  *   row_mask  [rows] uint8, NULL = all rows count.  A row whose entry is 0 (padding) does not count, and neither does a
  *             row whose logits are all -infinity: its logits (if masked) are not read, its picks are not counted, its
  *             floating outputs and its gradient are 0, its alternatives -1.
- *   temperature  tau > 0, finite: z = logits / tau, p = softmax(z) over the row, lse = log sum exp z.
+ *   temperature  tau, within 2^-100 .. 2^100: z = logits / tau, p = softmax(z) over the row, lse = log sum exp z.
  *   d_logits  the gradient, type `dtype`, row r at d_logits + r*ld_d, ld_d >= E; not the same memory as logits.  Places
  *             between the rows are left as they are.  accumulate = 0: overwritten; 1: added to what is there (each
  *             sum rounded to `dtype`; rows that do not count are left as they are).
  *   An index outside [0,E) is ignored.
  * Limits: E <= 1024, k, m and K <= E, m and K <= 64, rows < 2^31, ld and ld_d <= 2^31.  rows may be 0 (nothing is written but the groups' outputs).
- * Errors: NULL_PTR, INVALID_ARG (sizes, ld < E, unknown dtype, temperature not positive and finite, accumulate not 0 or 1,
+ * Errors: NULL_PTR, INVALID_ARG (sizes, ld < E, unknown dtype, temperature out of range, accumulate not 0 or 1,
  * d_logits == logits), UNSUPPORTED (limits), WORKSPACE.
  * ------------------------------------------------------------------------------------------- */
 typedef enum railsched_dtype { RAILSCHED_F32 = 0, RAILSCHED_BF16 = 1, RAILSCHED_F16 = 2 } railsched_dtype;

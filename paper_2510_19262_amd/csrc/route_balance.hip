@@ -59,7 +59,7 @@ __global__ __launch_bounds__(256) void route_balance_kernel(const T *__restrict_
             const bool live = row < hi && (!row_mask || row_mask[row] != 0);
             float t[VPL], e[VPL];
             row_values<T, LANES, VPL, VEC>(logits + row * ld, live, E, q, t);
-            const RowSoft soft = row_softmax<LANES, VPL>(t, e, 1.0f);
+            const RowSoft soft = row_softmax<LANES, VPL>(t, e, kLog2e);
             if (soft.total != 0.0f) {
                 const float scale = 1.0f / soft.total;
 #pragma unroll
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
             const bool live = there && (!row_mask || row_mask[row] != 0);
             float t[VPL], e[VPL];
             row_values<T, LANES, VPL, VEC>(logits + row * ld, live, E, q, t);
-            const RowSoft soft = row_softmax<LANES, VPL>(t, e, 1.0f);
+            const RowSoft soft = row_softmax<LANES, VPL>(t, e, kLog2e);
             const bool counts_here = soft.total != 0.0f;
             const float scale = 1.0f / soft.total;
             float ap = 0.0f;

@@ -14,36 +14,35 @@ namespace rs {
 // e^d - 1 - d: a series near 0, where the difference cancels.  |d| < 1/2: d^2/2 (1 + d/3 (1 + d/4 (... (1 + d/10)))), next term below 2^-27 of it
 __device__ __forceinline__ float exp_above(float d)
 {
-    float s = 1.0f + d * (1.0f / 10);
-    s = 1.0f + d * (1.0f / 9) * s;
-    s = 1.0f + d * (1.0f / 8) * s;
-    s = 1.0f + d * (1.0f / 7) * s;
-    s = 1.0f + d * (1.0f / 6) * s;
-    s = 1.0f + d * (1.0f / 5) * s;
-    s = 1.0f + d * (1.0f / 4) * s;
-    s = 1.0f + d * (1.0f / 3) * s;
+    float s = fmaf(d, 1.0f / 10, 1.0f);
+    s = fmaf(d * (1.0f / 9), s, 1.0f);
+    s = fmaf(d * (1.0f / 8), s, 1.0f);
+    s = fmaf(d * (1.0f / 7), s, 1.0f);
+    s = fmaf(d * (1.0f / 6), s, 1.0f);
+    s = fmaf(d * (1.0f / 5), s, 1.0f);
+    s = fmaf(d * (1.0f / 4), s, 1.0f);
+    s = fmaf(d * (1.0f / 3), s, 1.0f);
     s *= 0.5f * d * d;
-    return fabsf(d) < 0.5f ? s : expf(d) - 1.0f - d;
+    return fabsf(d) < 0.5f ? s : pow2(d * kLog2e) - 1.0f - d;
 }
-// x - log(1 + x), x > -1, the same way: x^2 (1/2 - x/3 + x^2/4 - ...); |x| < 1/8: nine terms, next one below 2^-27
+// x - log(1 + x), x > -1, the same way: with w = x / (2 + x), log(1 + x) = 2 (w + w^3/3 + w^5/5 + ...) and x - 2 w = x w.  |x| < 1/2: w^2 < 1/9, next
+// term below 2^-26 of it
 __device__ __forceinline__ float above_log(float x)
 {
-    float s = 1.0f / 10;
-    s = 1.0f / 9 - x * s;
-    s = 1.0f / 8 - x * s;
-    s = 1.0f / 7 - x * s;
-    s = 1.0f / 6 - x * s;
-    s = 1.0f / 5 - x * s;
-    s = 1.0f / 4 - x * s;
-    s = 1.0f / 3 - x * s;
-    s = 1.0f / 2 - x * s;
-    return fabsf(x) < 0.125f ? s * x * x : x - log1pf(x);
+    const float w = x / (2.0f + x), v = w * w;
+    float s = fmaf(v, 1.0f / 15, 1.0f / 13);
+    s = fmaf(v, s, 1.0f / 11);
+    s = fmaf(v, s, 1.0f / 9);
+    s = fmaf(v, s, 1.0f / 7);
+    s = fmaf(v, s, 1.0f / 5);
+    s = fmaf(v, s, 1.0f / 3);
+    return fabsf(x) < 0.5f ? w * (x - 2.0f * v * s) : x - kLn2 * log2_of(1.0f + x);
 }
 
 // What both passes need of a row.
 template <int LANES, int VPL, int NK>
 struct Distilled {
-    float t[VPL], e[VPL];        // the student: z - top, e^(z - top)
+    float y[VPL], e[VPL];        // the student: y, 2^y
     RowSoft soft;
     int at[NK];                  // this lane's entries: expert or -1
     bool again[NK];              // an entry whose expert another entry of the list names too
@@ -61,51 +60,69 @@ __device__ __forceinline__ void distill_row(const T *__restrict__ logits, int64_
                                             const float *__restrict__ t_lse, int K, int q0, float *mine, Distilled<LANES, VPL, NK> &o)
 {
     const T *__restrict__ from = logits + row * ld;
-    row_values<T, LANES, VPL, VEC>(from, live, E, q0, o.t);
+    row_values<T, LANES, VPL, VEC>(from, live, E, q0, o.y);
     float tl[NK], xl[NK];
     float best = -INFINITY;
     bool any = false;
 #pragma unroll
     for (int r = 0; r < NK; ++r) {
-        const int j = q0 + LANES * r;
-        const bool has = live && j < K;
-        o.at[r] = has ? t_idx[row * K + j] : -1;
-        tl[r] = has ? t_logit[row * K + j] : -INFINITY;
-        if (o.at[r] < 0 || o.at[r] >= E || tl[r] == -INFINITY) { o.at[r] = -1; tl[r] = -INFINITY; }
-        xl[r] = o.at[r] >= 0 ? (float)from[o.at[r]] : 0.0f;
-        best = fmaxf(best, tl[r]);
-        any |= o.at[r] >= 0;
+        o.at[r] = -1;
+        tl[r] = -INFINITY;
+        xl[r] = 0.0f;
+        if (LANES * r < K) {                             // the same for every lane: entries that no lane has cost nothing
+            const int j = q0 + LANES * r;
+            if (live && j < K) {
+                o.at[r] = t_idx[row * K + j];
+                tl[r] = t_logit[row * K + j];
+            }
+            if (o.at[r] < 0 || o.at[r] >= E || tl[r] == -INFINITY) { o.at[r] = -1; tl[r] = -INFINITY; }
+            if (o.at[r] >= 0) xl[r] = (float)from[o.at[r]];
+            best = fmaxf(best, tl[r]);
+            any |= o.at[r] >= 0;
+        }
     }
     o.listed = row_any<LANES>(any);
     lds_fill<LANES, VPL, VEC>(mine, q0, -1.0f);
     lds_order();
-    lds_mark<LANES, NK>(mine, q0, o.at, o.again);
-    o.soft = row_softmax<LANES, VPL>(o.t, o.e, inv_tau);
-    const float log_total = logf(o.soft.total), scale = 1.0f / o.soft.total;
-    best = row_max<LANES>(best);
-    // log of the teacher's total mass, in the same units as z
+    lds_mark<LANES, NK>(mine, q0, K, o.at, o.again);
+    const float c = inv_tau * kLog2e;
+    o.soft = row_softmax<LANES, VPL>(o.y, o.e, c);
+    const float scale = 1.0f / o.soft.total;
+    const float lse = fmaf(o.soft.largest, inv_tau, kLn2 * log2_of(o.soft.total));
+    // q, and the logarithm of the teacher's total mass
     float log_mass;
     if (t_lse) {
         log_mass = live ? t_lse[row] : 0.0f;
+#pragma unroll
+        for (int r = 0; r < NK; ++r) o.q[r] = LANES * r < K && o.at[r] >= 0 ? pow2(kLog2e * fmaf(tl[r], inv_tau, -log_mass)) : 0.0f;
     } else {
+        best = row_max<LANES>(best);
         float s = 0.0f;
 #pragma unroll
-        for (int r = 0; r < NK; ++r) s += o.at[r] >= 0 ? expf((tl[r] - best) * inv_tau) : 0.0f;
-        log_mass = best * inv_tau + logf(row_sum<LANES>(s));
+        for (int r = 0; r < NK; ++r) {
+            o.q[r] = LANES * r < K && o.at[r] >= 0 ? pow2(c * (tl[r] - best)) : 0.0f;
+            s += o.q[r];
+        }
+        s = row_sum<LANES>(s);
+        log_mass = fmaf(best, inv_tau, kLn2 * log2_of(s));
+        const float share = 1.0f / s;
+#pragma unroll
+        for (int r = 0; r < NK; ++r) o.q[r] = LANES * r < K && o.at[r] >= 0 ? o.q[r] * share : 0.0f;
     }
-    const float shift = (log_mass - o.soft.top) - log_total;
+    const float shift = log_mass - lse;
     float mass = 0.0f, gap = 0.0f;
 #pragma unroll
     for (int r = 0; r < NK; ++r) {
-        const bool has = o.at[r] >= 0;
-        o.q[r] = has ? expf(tl[r] * inv_tau - log_mass) : 0.0f;
-        o.p[r] = has ? exp_of(xl[r] * inv_tau - o.soft.top) * scale : 0.0f;
-        o.d[r] = (xl[r] - tl[r]) * inv_tau + shift;
-        mass += o.q[r];
-        gap += o.q[r] - (o.again[r] ? 0.0f : o.p[r]);
+        o.p[r] = o.d[r] = 0.0f;
+        if (LANES * r < K) {
+            o.p[r] = o.at[r] >= 0 ? pow2(o.soft.y(xl[r], c)) * scale : 0.0f;
+            o.d[r] = fmaf(xl[r] - tl[r], inv_tau, shift);
+            mass += o.q[r];
+            gap += o.q[r] - (o.again[r] ? 0.0f : o.p[r]);
+        }
     }
     o.mass = t_lse ? row_sum<LANES>(mass) : 1.0f;
-    o.gap = row_sum<LANES>(gap);
+    o.gap = t_lse ? row_sum<LANES>(gap) : 0.0f;
     float marks[VPL], outside = 0.0f;
     lds_values<LANES, VPL, VEC>(mine, q0, marks);
 #pragma unroll
@@ -135,14 +152,14 @@ __global__ __launch_bounds__(256) void route_distill_kernel(const T *__restrict_
         float terms = 0.0f, twice = 0.0f;
 #pragma unroll
         for (int r = 0; r < NK; ++r) {
-            if (o.at[r] >= 0) {
+            if (LANES * r < K && o.at[r] >= 0) {
                 // q (e^d - 1 - d) where e^d does not carry it off, and p alone where q has vanished
                 terms += o.q[r] == 0.0f ? o.p[r] : o.d[r] < 1.0f ? o.q[r] * exp_above(o.d[r]) : o.p[r] - o.q[r] - o.q[r] * o.d[r];
                 if (o.again[r]) twice += o.p[r];
             }
         }
         terms = row_sum<LANES>(terms);
-        twice = row_sum<LANES>(twice);
+        if (__ballot(twice != 0.0f) != 0ull) twice = row_sum<LANES>(twice);
         // sum q + q_r - (sum of p over the entries and outside): p of an expert listed twice is in its terms twice
         float sum = terms - twice;
         if (o.rest_q > 0.0f) {
@@ -177,7 +194,7 @@ __global__ __launch_bounds__(256) void route_distill_backward_kernel(const T *__
         distill_row<T, LANES, VPL, VEC, NK>(logits, row, live, E, ld, inv_tau, t_idx, t_logit, t_lse, K, q0, mine, o);
         const bool counts = o.soft.total != 0.0f;
         lds_order();
-        lds_put<LANES, NK>(mine, q0, o.at, o.again, o.q);
+        lds_put<LANES, NK>(mine, q0, K, o.at, o.again, o.q);
         float listed[VPL];
         lds_values<LANES, VPL, VEC>(mine, q0, listed);
         lds_order();
@@ -189,9 +206,9 @@ __global__ __launch_bounds__(256) void route_distill_backward_kernel(const T *__
 #pragma unroll
         for (int j = 0; j < VPL; ++j) {
             const float g = listed[j] < 0.0f ? o.e[j] * outside : o.e[j] * inside - listed[j];
-            o.t[j] = counts && o.listed ? unit * g : 0.0f;
+            o.y[j] = counts && o.listed ? unit * g : 0.0f;
         }
-        if (there && (counts || !add)) row_store<T, LANES, VPL, VEC>(d_logits + row * ld_d, E, q0, add != 0, o.t);
+        if (there && (counts || !add)) row_store<T, LANES, VPL, VEC>(d_logits + row * ld_d, E, q0, add != 0, o.y);
     }
 }
 

@@ -1,8 +1,8 @@
 // Log probabilities of given experts with log-sum-exp, entropy and the most likely experts of every row, and their gradient.
 //
-// One pass over a row: the largest logit, then total = sum e^(z - top) and dot = sum e^(z - top) (z - top) from the values in
-// registers; lse = top + log total, entropy = log total - dot / total (no cancellation: both terms are >= 0), and the picks' logits are
-// read again, from the cache.
+// One pass over a row, in powers of two: the largest logit, then total = sum 2^y and dot = sum 2^y y from the values in registers (y <= 0: relative to the
+// largest).  lse = largest / tau + ln 2 log2 total, entropy = ln 2 (log2 total - dot / total) (no cancellation: both terms are >= 0), and the picks' logits
+// are read again, from the cache.
 #include "router_core.h"
 
 namespace rs {
@@ -22,23 +22,24 @@ __global__ __launch_bounds__(256) void route_logprobs_kernel(const T *__restrict
         const bool there = row < rows;
         const bool live = there && (!row_mask || row_mask[row] != 0);
         const T *__restrict__ from = logits + row * ld;
-        float raw[VPL], t[VPL], e[VPL];
+        float raw[VPL], y[VPL], e[VPL];
         row_values<T, LANES, VPL, VEC>(from, live, E, q, raw);
 #pragma unroll
-        for (int j = 0; j < VPL; ++j) t[j] = raw[j];
-        const RowSoft soft = row_softmax<LANES, VPL>(t, e, inv_tau);
-        const float dot = row_dot_t<LANES, VPL>(t, e);
+        for (int j = 0; j < VPL; ++j) y[j] = raw[j];
+        const float c = inv_tau * kLog2e;
+        const RowSoft soft = row_softmax<LANES, VPL>(y, e, c);
+        const float dot = row_dot<LANES, VPL>(y, e);
         const bool counts = soft.total != 0.0f;
-        const float log_total = logf(soft.total);
+        const float log_total = log2_of(soft.total);
         if (there && q == 0) {
-            if (lse) lse[row] = counts ? soft.top + log_total : 0.0f;
-            if (entropy) entropy[row] = counts ? log_total - dot / soft.total : 0.0f;
+            if (lse) lse[row] = counts ? fmaf(soft.largest, inv_tau, kLn2 * log_total) : 0.0f;
+            if (entropy) entropy[row] = counts ? kLn2 * (log_total - dot / soft.total) : 0.0f;
         }
         if (there) {
             for (int j = q; j < k; j += LANES) {
                 const int at = topk_idx[row * k + j];
                 const bool good = counts && at >= 0 && at < E;
-                logp[row * k + j] = good ? ((float)from[at] * inv_tau - soft.top) - log_total : 0.0f;
+                logp[row * k + j] = good ? kLn2 * (soft.y((float)from[at], c) - log_total) : 0.0f;
             }
         }
         for (int sel = 0; sel < m; ++sel) {
@@ -55,14 +56,14 @@ __global__ __launch_bounds__(256) void route_logprobs_kernel(const T *__restrict
             for (int j = 0; j < VPL; ++j) raw[j] = slot_index<LANES, VPL, VEC>(q, j) == at ? -INFINITY : raw[j];
             if (there && q == sel % LANES) {
                 alt_idx[row * m + sel] = at < E ? at : -1;
-                alt_logp[row * m + sel] = !counts ? 0.0f : at < E ? (best * inv_tau - soft.top) - log_total : -INFINITY;
+                alt_logp[row * m + sel] = !counts ? 0.0f : at < E ? kLn2 * (soft.y(best, c) - log_total) : -INFINITY;
             }
         }
     }
 }
 
-// d_logits[e] = (sum of d_logp over the slots of e - p_e (sum of d_logp - d_lse + d_entropy (log p_e + entropy))) / tau.  The slots' gradients
-// reach the lanes that hold their experts through a row in LDS.
+// d_logits[e] = (sum of d_logp over the slots of e - p_e (sum of d_logp - d_lse + d_entropy (log p_e + entropy))) / tau, where log p_e + entropy is
+// ln 2 (y_e - sum p y): the logarithm of the total is in both.  The slots' gradients reach the lanes that hold their experts through a row in LDS.
 template <typename T, int LANES, int VPL, bool VEC, int NK>
 __global__ __launch_bounds__(256) void route_logprobs_backward_kernel(const T *__restrict__ logits, int64_t rows, int E, int64_t ld,
                                                                       float inv_tau, const uint8_t *__restrict__ row_mask,
@@ -80,9 +81,9 @@ __global__ __launch_bounds__(256) void route_logprobs_backward_kernel(const T *_
         const int64_t row = w0 + threadIdx.x / LANES;
         const bool there = row < rows;
         const bool live = there && (!row_mask || row_mask[row] != 0);
-        float t[VPL], e[VPL];
-        row_values<T, LANES, VPL, VEC>(logits + row * ld, live, E, q, t);
-        const RowSoft soft = row_softmax<LANES, VPL>(t, e, inv_tau);
+        float y[VPL], e[VPL];
+        row_values<T, LANES, VPL, VEC>(logits + row * ld, live, E, q, y);
+        const RowSoft soft = row_softmax<LANES, VPL>(y, e, inv_tau * kLog2e);
         const bool counts = soft.total != 0.0f;
 
         float dx[VPL], sum = 0.0f;
@@ -103,8 +104,8 @@ __global__ __launch_bounds__(256) void route_logprobs_backward_kernel(const T *_
                 }
                 lds_fill<LANES, VPL, VEC>(mine, q, 0.0f);
                 lds_order();
-                lds_mark<LANES, NK>(mine, q, at, again);
-                lds_put<LANES, NK>(mine, q, at, again, g);
+                lds_mark<LANES, NK>(mine, q, k - first, at, again);
+                lds_put<LANES, NK>(mine, q, k - first, at, again, g);
                 lds_values<LANES, VPL, VEC>(mine, q, part);
                 lds_order();
 #pragma unroll
@@ -115,11 +116,10 @@ __global__ __launch_bounds__(256) void route_logprobs_backward_kernel(const T *_
         const float pull = sum - (d_lse && live ? d_lse[row] : 0.0f);
         const float scale = 1.0f / soft.total;
         if (d_entropy) {
-            const float log_total = logf(soft.total);
-            const float h = log_total - row_dot_t<LANES, VPL>(t, e) * scale;
-            const float gh = live ? d_entropy[row] : 0.0f;
+            const float mean = row_dot<LANES, VPL>(y, e) * scale;
+            const float gh = live ? kLn2 * d_entropy[row] : 0.0f;
 #pragma unroll
-            for (int j = 0; j < VPL; ++j) dx[j] -= e[j] * scale * (pull + gh * ((fmaxf(t[j], -1e30f) - log_total) + h));
+            for (int j = 0; j < VPL; ++j) dx[j] -= e[j] * scale * (pull + gh * (fmaxf(y[j], -1e30f) - mean));
         } else {
 #pragma unroll
             for (int j = 0; j < VPL; ++j) dx[j] -= e[j] * scale * pull;

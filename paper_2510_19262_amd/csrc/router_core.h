@@ -116,45 +116,45 @@ __device__ __forceinline__ void row_store(T *__restrict__ row, int E, int q, boo
     }
 }
 
-// exp(t) by the hardware's power of two: t <= 0, so the rounding of t * log2(e) is at most |t| 2^-24 of a value e^t, below 2^-25 of the
-// row's largest
-__device__ __forceinline__ float exp_of(float t) { return __builtin_amdgcn_exp2f(t * 1.44269504088896341f); }
+// Everything about a row is done in powers of two: with c = log2(e) / tau, y = c (logit - largest) and the hardware's 2^y.  y is 0 for the largest logit,
+// exactly, and no finite logits overflow; 2^y is off by about 2 |y| 2^-24 of itself: at most about 2^-24 of the row's largest.
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+__device__ __forceinline__ float pow2(float y) { return __builtin_amdgcn_exp2f(y); }
+__device__ __forceinline__ float log2_of(float v) { return __builtin_amdgcn_logf(v); }       // of normal numbers, to one step
 
-// Softmax of a row: x holds the logits on entry and t = z - max z on return, e the exponentials of t.
+// Softmax of a row: x holds the logits on entry and y on return, e the powers.
 struct RowSoft {
-    float top;      // the largest z (0 in a row without one)
+    float largest;  // logit (0 in a row without one)
     float total;    // sum of e: at least 1, or 0 in a row that does not count (every logit -infinity), or NaN
+    __device__ __forceinline__ float y(float logit, float c) const { return c * (logit - largest); }
 };
 template <int LANES, int VPL>
-__device__ __forceinline__ RowSoft row_softmax(float (&x)[VPL], float (&e)[VPL], float inv_tau)
+__device__ __forceinline__ RowSoft row_softmax(float (&x)[VPL], float (&e)[VPL], float c)
 {
     RowSoft r;
-    float m = -INFINITY;
+    float m = x[0];
 #pragma unroll
-    for (int j = 0; j < VPL; ++j) {
-        x[j] *= inv_tau;
-        m = fmaxf(m, x[j]);
-    }
+    for (int j = 1; j < VPL; ++j) m = fmaxf(m, x[j]);
     m = row_max<LANES>(m);
-    r.top = m == -INFINITY ? 0.0f : m;
+    r.largest = m == -INFINITY ? 0.0f : m;
     float s = 0.0f;
 #pragma unroll
     for (int j = 0; j < VPL; ++j) {
-        x[j] -= r.top;
-        e[j] = exp_of(x[j]);
+        x[j] = r.y(x[j], c);
+        e[j] = pow2(x[j]);
         s += e[j];
     }
     r.total = row_sum<LANES>(s);
     return r;
 }
 
-// sum of e t over the row (e 0 where t is -infinity: the product is 0 there)
+// sum of e y over the row (e 0 where y is -infinity: the product is 0 there)
 template <int LANES, int VPL>
-__device__ __forceinline__ float row_dot_t(const float (&t)[VPL], const float (&e)[VPL])
+__device__ __forceinline__ float row_dot(const float (&y)[VPL], const float (&e)[VPL])
 {
     float a = 0.0f;
 #pragma unroll
-    for (int j = 0; j < VPL; ++j) a += e[j] * fmaxf(t[j], -1e30f);
+    for (int j = 0; j < VPL; ++j) a += e[j] * fmaxf(y[j], -1e30f);
     return row_sum<LANES>(a);
 }
 
@@ -190,23 +190,23 @@ __device__ __forceinline__ void lds_values(const float *row, int q, float (&x)[V
     }
 }
 
-// Marks the places at[r] (-1: none) of this lane's entries q, q + LANES, ... in the row; on return again[r] says that another entry of the same
+// Marks the places at[r] (-1: none) of this lane's entries q, q + LANES, ... of `count` in the row; on return again[r] says that another entry of the same
 // place holds it (of several entries with one place exactly one is not `again`).  The marked places hold values >= 0.
 template <int LANES, int N>
-__device__ __forceinline__ void lds_mark(float *row, int q, const int (&at)[N], bool (&again)[N])
+__device__ __forceinline__ void lds_mark(float *row, int q, int count, const int (&at)[N], bool (&again)[N])
 {
 #pragma unroll
     for (int r = 0; r < N; ++r)
-        if (at[r] >= 0) row[at[r]] = (float)(q + LANES * r);
+        if (LANES * r < count && at[r] >= 0) row[at[r]] = (float)(q + LANES * r);
     lds_order();
 #pragma unroll
-    for (int r = 0; r < N; ++r) again[r] = at[r] >= 0 && row[at[r]] != (float)(q + LANES * r);
+    for (int r = 0; r < N; ++r) again[r] = LANES * r < count && at[r] >= 0 && row[at[r]] != (float)(q + LANES * r);
     lds_order();
 }
 
 // Puts value[r] at the marked places; entries of one place are added up in the order of the entries, so that equal inputs give equal bits.
 template <int LANES, int N>
-__device__ __forceinline__ void lds_put(float *row, int q, const int (&at)[N], const bool (&again)[N], const float (&value)[N])
+__device__ __forceinline__ void lds_put(float *row, int q, int count, const int (&at)[N], const bool (&again)[N], const float (&value)[N])
 {
     bool any = false;
 #pragma unroll
@@ -214,18 +214,19 @@ __device__ __forceinline__ void lds_put(float *row, int q, const int (&at)[N], c
     if (__ballot(any) == 0ull) {
 #pragma unroll
         for (int r = 0; r < N; ++r)
-            if (at[r] >= 0) row[at[r]] = value[r];
+            if (LANES * r < count && at[r] >= 0) row[at[r]] = value[r];
     } else {                                             // an expert listed twice: one entry after the other
 #pragma unroll
         for (int r = 0; r < N; ++r)
-            if (at[r] >= 0) row[at[r]] = 0.0f;
+            if (LANES * r < count && at[r] >= 0) row[at[r]] = 0.0f;
         lds_order();
 #pragma unroll
         for (int r = 0; r < N; ++r)
-            for (int i = 0; i < LANES; ++i) {
-                if (q == i && at[r] >= 0) row[at[r]] += value[r];
-                lds_order();
-            }
+            if (LANES * r < count)
+                for (int i = 0; i < LANES; ++i) {
+                    if (q == i && at[r] >= 0) row[at[r]] += value[r];
+                    lds_order();
+                }
     }
     lds_order();
 }
@@ -234,7 +235,7 @@ __device__ __forceinline__ void lds_put(float *row, int q, const int (&at)[N], c
 inline int check_router(const void *logits, int32_t dtype, int64_t rows, int32_t E, int64_t ld, float temperature)
 {
     if (dtype < RAILSCHED_F32 || dtype > RAILSCHED_F16 || rows < 0 || E < 1 || ld < E) return RAILSCHED_ERR_INVALID_ARG;
-    if (!(temperature > 0.0f) || !(temperature <= 3.402823466e38f)) return RAILSCHED_ERR_INVALID_ARG;
+    if (!(temperature >= 0x1p-100f) || !(temperature <= 0x1p100f)) return RAILSCHED_ERR_INVALID_ARG;
     if (E > kMaxExperts || rows > 0x7FFFFFFFll || ld > (int64_t(1) << 31)) return RAILSCHED_ERR_UNSUPPORTED;
     if (rows > 0 && !logits) return RAILSCHED_ERR_NULL_PTR;
     return RAILSCHED_OK;
