@@ -26,22 +26,67 @@ struct Groups {
     }
 };
 
-struct Record {             // of a part: E sums, E counts, the rows that count
-    static __host__ __device__ int64_t words(int E) { return 2 * (int64_t)E + 1; }
+// The workspace: a record for every part (E sums, E counts, the rows that count), the tickets of the groups, and the products of their column tiles.
+struct Records {
+    float *data;
+    unsigned *tickets;
+    double *dots;
+    int64_t words;
+    __device__ __forceinline__ float *at(int64_t slice, int64_t group) const { return data + (slice + group) * words; }
 };
 
-template <typename T, int LANES, int VPL, bool VEC>
+constexpr int kTile = 32;                               // columns that a workgroup of the joining kernel adds up
+
+// v added up over the lanes that are a multiple of LANES away from this one, in all of them
+template <int LANES>
+__device__ __forceinline__ float rows_sum(float v)
+{
+    if constexpr (LANES <= 2) v += xlane<2>(v);
+    if constexpr (LANES <= 4) v += __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(v), 0x101F));     // lane ^ 4
+    if constexpr (LANES <= 8) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xF, 0xF, false));   // row_ror:8, lane ^ 8
+    if constexpr (LANES <= 16) v += xlane<16>(v);
+    if constexpr (LANES <= 32) v += xlane<32>(v);
+    return v;
+}
+
+// sum over the workgroup of 64 * WAVES threads, in thread 0; the order is fixed
+template <int WAVES>
+__device__ __forceinline__ double block_sum(double v, double *part)
+{
+#pragma unroll
+    for (int w = 32; w >= 1; w /= 2) v += __shfl_down(v, w);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    double s = 0.0;
+    if (threadIdx.x == 0) {
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) s += part[w];
+    }
+    return s;
+}
+__device__ __forceinline__ float balance_loss(float coef, int E, int k, int64_t n, double dot)
+{
+    return n ? (float)((double)coef * E / ((double)k * n * n) * dot) : 0.0f;
+}
+
+// DIRECT: every slice is a whole group, whose outputs leave from here.
+template <typename T, int LANES, int VPL, bool VEC, bool DIRECT>
 __global__ __launch_bounds__(256) void route_balance_kernel(const T *__restrict__ logits, int E, int64_t ld, const uint8_t *__restrict__ row_mask,
-                                                            const int32_t *__restrict__ topk_idx, int k, Groups groups, int64_t slice_rows,
-                                                            float *__restrict__ records)
+                                                            const int32_t *__restrict__ topk_idx, int k, Groups groups, int64_t slice_rows, float coef,
+                                                            Records records, int64_t *__restrict__ counts, int64_t *__restrict__ tokens,
+                                                            float *__restrict__ prob_sum, float *__restrict__ loss)
 {
     constexpr int ROWS_PER_BLOCK = 256 / LANES;
-    __shared__ __align__(16) float sums[ROWS_PER_BLOCK * LANES * VPL];
-    __shared__ unsigned picks[kMaxExperts];
+    __shared__ float sums[4][LANES * VPL];
+    __shared__ unsigned picks[LANES * VPL];
     __shared__ unsigned counted;
-    const int q = threadIdx.x % LANES, slot = threadIdx.x / LANES;
+    __shared__ double part[4];
+    const int q = threadIdx.x % LANES, slot = threadIdx.x / LANES, wave = threadIdx.x >> 6;
     const int64_t r0 = blockIdx.x * slice_rows;
     const int64_t r1 = r0 + slice_rows < groups.rows ? r0 + slice_rows : groups.rows;
+    if constexpr (!DIRECT) {
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < groups.n; i += (int64_t)gridDim.x * 256) records.tickets[i] = 0;
+    }
     for (int g = groups.first(r0); g < groups.n; ++g) {
         const int64_t gb = groups.begin(g), ge = groups.begin(g + 1);
         if (gb >= r1) break;
@@ -73,52 +118,94 @@ __global__ __launch_bounds__(256) void route_balance_kernel(const T *__restrict_
         }
         if (here) atomicAdd(&counted, here);
 #pragma unroll
-        for (int j = 0; j < VPL; ++j) sums[slot * (LANES * VPL) + slot_index<LANES, VPL, VEC>(q, j)] = acc[j];
-        __syncthreads();
-        float *rec = records + (blockIdx.x + (int64_t)g) * Record::words(E);
-        for (int i = threadIdx.x; i < E; i += 256) {
-            float s = 0.0f;
-            for (int r = 0; r < ROWS_PER_BLOCK; ++r) s += sums[r * (LANES * VPL) + i];
-            rec[i] = s;
-            reinterpret_cast<unsigned *>(rec)[E + i] = picks[i];
+        for (int j = 0; j < VPL; ++j) {
+            const float s = rows_sum<LANES>(acc[j]);
+            if ((threadIdx.x & 63) < LANES) sums[wave][slot_index<LANES, VPL, VEC>(q, j)] = s;
         }
-        if (threadIdx.x == 0) reinterpret_cast<unsigned *>(rec)[2 * E] = counted;
+        __syncthreads();
+        if constexpr (DIRECT) {
+            double dot = 0.0;
+            for (int i = threadIdx.x; i < E; i += 256) {
+                const float s = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
+                prob_sum[(int64_t)g * E + i] = s;
+                counts[(int64_t)g * E + i] = picks[i];
+                dot += (double)s * picks[i];
+            }
+            dot = block_sum<4>(dot, part);
+            if (threadIdx.x == 0) {
+                tokens[g] = counted;
+                loss[g] = balance_loss(coef, E, k, counted, dot);
+            }
+        } else {
+            float *rec = records.at(blockIdx.x, g);
+            for (int i = threadIdx.x; i < E; i += 256) {
+                rec[i] = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
+                reinterpret_cast<unsigned *>(rec)[E + i] = picks[i];
+            }
+            if (threadIdx.x == 0) reinterpret_cast<unsigned *>(rec)[2 * E] = counted;
+        }
         __syncthreads();
     }
 }
 
-__global__ __launch_bounds__(256) void route_balance_join_kernel(const float *__restrict__ records, int E, int k, Groups groups, int64_t slice_rows,
-                                                                 float coef, int64_t *__restrict__ counts, int64_t *__restrict__ tokens,
-                                                                 float *__restrict__ prob_sum, float *__restrict__ loss)
+// Adds the records of a group up: a workgroup takes kTile columns at a time (all of them, or one tile in a grid of tiles), its threads rows of records.
+// The last tile of a group to arrive forms the loss from the tiles' products, in the order of the tiles.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void route_balance_join_kernel(Records records, int E, int k, Groups groups, int64_t slice_rows, float coef,
+                                                                     int64_t *__restrict__ counts, int64_t *__restrict__ tokens,
+                                                                     float *__restrict__ prob_sum, float *__restrict__ loss)
 {
-    __shared__ double part[256];
-    const int g = blockIdx.x;
+    constexpr int LINES = THREADS / kTile;
+    __shared__ double sums[LINES][kTile];
+    __shared__ int64_t picks[LINES][kTile];
+    __shared__ double part[THREADS / 64];
+    const int g = blockIdx.x, tiles = gridDim.y;
+    const int col = threadIdx.x % kTile, line = threadIdx.x / kTile;
     const int64_t gb = groups.begin(g), ge = groups.begin(g + 1);
     const int64_t s0 = gb / slice_rows, s1 = gb < ge ? (ge - 1) / slice_rows + 1 : s0;
-    const int64_t words = Record::words(E);
-    double dot = 0.0;
-    for (int i = threadIdx.x; i < E; i += 256) {
+    double dot = 0.0, n = 0.0;
+    for (int i0 = blockIdx.y * kTile; i0 < E; i0 += tiles * kTile) {
+        const int i = i0 + col;
         double s = 0.0;
         int64_t c = 0;
-        for (int64_t r = s0; r < s1; ++r) {
-            const float *rec = records + (r + g) * words;
-            s += rec[i];
-            c += reinterpret_cast<const unsigned *>(rec)[E + i];
+        if (i < E) {
+#pragma unroll 8
+            for (int64_t r = s0 + line; r < s1; r += LINES) {
+                const float *rec = records.at(r, g);
+                s += rec[i];
+                c += reinterpret_cast<const unsigned *>(rec)[E + i];
+            }
         }
-        prob_sum[(int64_t)g * E + i] = (float)s;
-        counts[(int64_t)g * E + i] = c;
-        dot += s * (double)c;
+        sums[line][col] = s;
+        picks[line][col] = c;
+        __syncthreads();
+        if (line == 0 && i < E) {
+#pragma unroll
+            for (int l = 1; l < LINES; ++l) {
+                s += sums[l][col];
+                c += picks[l][col];
+            }
+            prob_sum[(int64_t)g * E + i] = (float)s;
+            counts[(int64_t)g * E + i] = c;
+            dot += s * (double)c;
+        }
+        __syncthreads();
     }
-    part[threadIdx.x] = dot;
+    for (int64_t r = s0 + threadIdx.x; r < s1; r += THREADS) n += reinterpret_cast<const unsigned *>(records.at(r, g))[2 * E];
+    dot = block_sum<THREADS / 64>(dot, part);
     __syncthreads();
-    if (threadIdx.x == 0) {
-        double sum = 0.0;
-        for (int i = 0; i < 256; ++i) sum += part[i];
-        int64_t n = 0;
-        for (int64_t r = s0; r < s1; ++r) n += reinterpret_cast<const unsigned *>(records + (r + g) * words)[2 * E];
-        tokens[g] = n;
-        loss[g] = n ? (float)((double)coef * E / ((double)k * n * n) * sum) : 0.0f;
+    n = block_sum<THREADS / 64>(n, part);
+    if (threadIdx.x != 0) return;
+    if (tiles > 1) {
+        double *dots = records.dots + (int64_t)g * tiles;
+        __hip_atomic_store(&dots[blockIdx.y], dot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const unsigned ticket = __hip_atomic_fetch_add(&records.tickets[g], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+        if (ticket != (unsigned)tiles - 1) return;
+        dot = 0.0;
+        for (int t = 0; t < tiles; ++t) dot += __hip_atomic_load(&dots[t], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
+    tokens[g] = (int64_t)n;
+    loss[g] = balance_loss(coef, E, k, (int64_t)n, dot);
 }
 
 // d_logits[e] = p_e (a_e - sum_f a_f p_f), a_e = d_loss coef E c_e / (k n^2).  The gradient does not change with a constant added to a: the mean
@@ -131,8 +218,8 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
                                                                      int add, T *__restrict__ d_logits, int64_t ld_d)
 {
     constexpr int ROWS_PER_BLOCK = 256 / LANES;
-    __shared__ double part[256];
-    __shared__ float weight[kMaxExperts];
+    __shared__ double part[4], total;
+    __shared__ float weight[LANES * VPL];
     const int q = threadIdx.x % LANES, slot = threadIdx.x / LANES;
     const int64_t r0 = blockIdx.x * slice_rows;
     const int64_t r1 = r0 + slice_rows < groups.rows ? r0 + slice_rows : groups.rows;
@@ -144,14 +231,10 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
         const int64_t *__restrict__ c = counts + (int64_t)g * E;
         double sum = 0.0;
         for (int i = threadIdx.x; i < E; i += 256) sum += (double)c[i];
-        part[threadIdx.x] = sum;
+        sum = block_sum<4>(sum, part);
+        if (threadIdx.x == 0) total = sum;
         __syncthreads();
-#pragma unroll
-        for (int w = 128; w >= 1; w /= 2) {
-            if (threadIdx.x < w) part[threadIdx.x] += part[threadIdx.x + w];
-            __syncthreads();
-        }
-        const double mean = part[0] / E, n = (double)tokens[g];
+        const double mean = total / E, n = (double)tokens[g];
         const double unit = n > 0.0 ? (double)d_loss[g] * coef * E / ((double)k * n * n) : 0.0;
         for (int i = threadIdx.x; i < E; i += 256) weight[i] = (float)(unit * ((double)c[i] - mean));
         __syncthreads();
@@ -193,6 +276,13 @@ static int64_t balance_slice_rows(int64_t rows, int E)
     return r > least ? r : least;
 }
 static int64_t balance_slices(int64_t rows, int E) { return (rows + balance_slice_rows(rows, E) - 1) / balance_slice_rows(rows, E); }
+static int balance_tiles(int E) { return (E + kTile - 1) / kTile; }
+
+static size_t records_bytes(int64_t rows, int32_t groups, int32_t E)
+{
+    return align_up((size_t)(balance_slices(rows, E) + groups + 1) * (2 * (size_t)E + 1) * sizeof(float), 256);
+}
+static size_t tickets_bytes(int32_t groups) { return align_up((size_t)groups * sizeof(unsigned), 256); }
 
 static int check_groups(int64_t rows, const int64_t *group_off, int32_t groups)
 {
@@ -215,7 +305,7 @@ extern "C" size_t railsched_route_balance_workspace_bytes(int64_t rows, int32_t 
 {
     using namespace rs;
     if (rows < 0 || rows > 0x7FFFFFFFll || groups < 0 || E < 1 || E > kMaxExperts) return 0;
-    return align_up((size_t)(balance_slices(rows, E) + groups + 1) * Record::words(E) * sizeof(float), 256);
+    return records_bytes(rows, groups, E) + tickets_bytes(groups) + align_up((size_t)groups * balance_tiles(E) * sizeof(double), 256);
 }
 
 extern "C" int railsched_route_balance(const void *logits, int32_t dtype, int64_t rows, int32_t E, int64_t ld, const uint8_t *row_mask,
@@ -232,22 +322,39 @@ extern "C" int railsched_route_balance(const void *logits, int32_t dtype, int64_
     if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 != 0 || ws_bytes < railsched_route_balance_workspace_bytes(rows, groups, E)) return RAILSCHED_ERR_WORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const Groups gr = make_groups(rows, group_off, groups);
-    const int64_t slice_rows = balance_slice_rows(rows, E);
-    float *records = static_cast<float *>(ws);
+    // equal groups of few rows: a workgroup each, one launch and no records
+    const bool direct = !group_off && rows > 0 && gr.each * E <= 16384;
+    const int64_t slice_rows = direct ? gr.each : balance_slice_rows(rows, E);
+    Records records;
+    records.data = static_cast<float *>(ws);
+    records.words = 2 * (int64_t)E + 1;
+    records.tickets = reinterpret_cast<unsigned *>(static_cast<char *>(ws) + records_bytes(rows, groups, E));
+    records.dots = reinterpret_cast<double *>(reinterpret_cast<char *>(records.tickets) + tickets_bytes(groups));
     if (rows > 0) {
+        const dim3 grid((unsigned)((rows + slice_rows - 1) / slice_rows));
         const int rc = by_dtype(dtype, [&](auto t) {
             using T = decltype(t);
             return by_shape(E, in_fours<T>(logits, E, ld), [&](auto s) {
                 using S = decltype(s);
-                hipLaunchKernelGGL((route_balance_kernel<T, S::LANES, S::VPL, S::VEC>), dim3((unsigned)balance_slices(rows, E)), dim3(256), 0, st,
-                                   static_cast<const T *>(logits), E, ld, row_mask, topk_idx, k, gr, slice_rows, records);
+                if (direct)
+                    hipLaunchKernelGGL((route_balance_kernel<T, S::LANES, S::VPL, S::VEC, true>), grid, dim3(256), 0, st, static_cast<const T *>(logits), E,
+                                       ld, row_mask, topk_idx, k, gr, slice_rows, coef, records, counts, tokens, prob_sum, loss);
+                else
+                    hipLaunchKernelGGL((route_balance_kernel<T, S::LANES, S::VPL, S::VEC, false>), grid, dim3(256), 0, st, static_cast<const T *>(logits), E,
+                                       ld, row_mask, topk_idx, k, gr, slice_rows, coef, records, counts, tokens, prob_sum, loss);
                 return launch_status();
             });
         });
-        if (rc) return rc;
+        if (rc || direct) return rc;
     }
-    hipLaunchKernelGGL(route_balance_join_kernel, dim3((unsigned)groups), dim3(256), 0, st, records, E, k, gr, slice_rows, coef, counts, tokens, prob_sum,
-                       loss);
+    // a workgroup for every tile of columns where a group has many records; otherwise one for the group
+    const int64_t each = balance_slices(rows, E) / groups;
+    if (each > 16)
+        hipLaunchKernelGGL(route_balance_join_kernel<1024>, dim3((unsigned)groups, (unsigned)balance_tiles(E)), dim3(1024), 0, st, records, E, k, gr, slice_rows,
+                           coef, counts, tokens, prob_sum, loss);
+    else
+        hipLaunchKernelGGL(route_balance_join_kernel<256>, dim3((unsigned)groups), dim3(256), 0, st, records, E, k, gr, slice_rows, coef, counts, tokens,
+                           prob_sum, loss);
     return launch_status();
 }
 
