@@ -106,7 +106,7 @@ __global__ __launch_bounds__(256) void route_balance_kernel(const T *__restrict_
             row_values<T, LANES, VPL, VEC>(logits + row * ld, live, E, q, t);
             const RowSoft soft = row_softmax<LANES, VPL>(t, e, kLog2e);
             if (soft.total != 0.0f) {
-                const float scale = 1.0f / soft.total;
+                const float scale = inverse(soft.total);
 #pragma unroll
                 for (int j = 0; j < VPL; ++j) acc[j] += e[j] * scale;
                 here += q == 0;
@@ -252,7 +252,7 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
             row_values<T, LANES, VPL, VEC>(logits + row * ld, live, E, q, t);
             const RowSoft soft = row_softmax<LANES, VPL>(t, e, kLog2e);
             const bool counts_here = soft.total != 0.0f;
-            const float scale = 1.0f / soft.total;
+            const float scale = inverse(soft.total);
             float ap = 0.0f;
 #pragma unroll
             for (int j = 0; j < VPL; ++j) {

@@ -87,7 +87,7 @@ __device__ __forceinline__ void distill_row(const T *__restrict__ logits, int64_
     lds_mark<LANES, NK>(mine, q0, K, o.at, o.again);
     const float c = inv_tau * kLog2e;
     o.soft = row_softmax<LANES, VPL>(o.y, o.e, c);
-    const float scale = 1.0f / o.soft.total;
+    const float scale = inverse(o.soft.total);
     const float lse = fmaf(o.soft.largest, inv_tau, kLn2 * log2_of(o.soft.total));
     // q, and the logarithm of the teacher's total mass
     float log_mass;
@@ -105,7 +105,7 @@ __device__ __forceinline__ void distill_row(const T *__restrict__ logits, int64_
         }
         s = row_sum<LANES>(s);
         log_mass = fmaf(best, inv_tau, kLn2 * log2_of(s));
-        const float share = 1.0f / s;
+        const float share = inverse(s);
 #pragma unroll
         for (int r = 0; r < NK; ++r) o.q[r] = LANES * r < K && o.at[r] >= 0 ? o.q[r] * share : 0.0f;
     }
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(256) void route_distill_kernel(const T *__restrict_
         if (__ballot(twice != 0.0f) != 0ull) twice = row_sum<LANES>(twice);
         // sum q + q_r - (sum of p over the entries and outside): p of an expert listed twice is in its terms twice
         float sum = terms - twice;
-        if (o.rest_q > 0.0f) {
+        if (t_lse && o.rest_q > 0.0f) {
             const float apart = o.gap / o.rest_q;                        // p_r / q_r - 1
             sum += o.rest_q * above_log(apart);
         } else {
@@ -199,7 +199,7 @@ __global__ __launch_bounds__(256) void route_distill_backward_kernel(const T *__
         lds_values<LANES, VPL, VEC>(mine, q0, listed);
         lds_order();
         const float unit = live && o.listed ? tau * d_loss[row] : 0.0f;
-        const float scale = 1.0f / o.soft.total;
+        const float scale = inverse(o.soft.total);
         const float inside = (o.mass + o.rest_q) * scale;
         // Q + q_r - q_r / p_r is (p_r - q_r) / p_r where sum q + q_r is 1
         const float outside = (o.rest_q > 0.0f ? o.gap / o.rest_p : o.mass) * scale;
@@ -244,9 +244,11 @@ extern "C" int railsched_route_distill(const void *logits, int32_t dtype, int64_
         using T = decltype(t);
         return by_shape(E, in_fours<T>(logits, E, ld), [&](auto s) {
             using S = decltype(s);
-            return launch_distill(rows, S::LANES, [&](dim3 grid) {
-                hipLaunchKernelGGL((route_distill_kernel<T, S::LANES, S::VPL, S::VEC, list_regs<S>()>), grid, dim3(256), 0, st,
-                                   static_cast<const T *>(logits), rows, E, ld, temperature, row_mask, t_idx, t_logit, t_lse, K, loss);
+            return by_entries<S>(K, [&](auto n) {
+                return launch_distill(rows, S::LANES, [&](dim3 grid) {
+                    hipLaunchKernelGGL((route_distill_kernel<T, S::LANES, S::VPL, S::VEC, decltype(n)::value>), grid, dim3(256), 0, st,
+                                       static_cast<const T *>(logits), rows, E, ld, temperature, row_mask, t_idx, t_logit, t_lse, K, loss);
+                });
             });
         });
     });
@@ -268,10 +270,12 @@ extern "C" int railsched_route_distill_backward(const void *logits, int32_t dtyp
         using T = decltype(t);
         return by_shape(E, in_fours<T>(logits, E, ld) && in_fours<T>(d_logits, E, ld_d), [&](auto s) {
             using S = decltype(s);
-            return launch_distill(rows, S::LANES, [&](dim3 grid) {
-                hipLaunchKernelGGL((route_distill_backward_kernel<T, S::LANES, S::VPL, S::VEC, list_regs<S>()>), grid, dim3(256), 0, st,
-                                   static_cast<const T *>(logits), rows, E, ld, temperature, row_mask, t_idx, t_logit, t_lse, K, d_loss, accumulate,
-                                   static_cast<T *>(d_logits), ld_d);
+            return by_entries<S>(K, [&](auto n) {
+                return launch_distill(rows, S::LANES, [&](dim3 grid) {
+                    hipLaunchKernelGGL((route_distill_backward_kernel<T, S::LANES, S::VPL, S::VEC, decltype(n)::value>), grid, dim3(256), 0, st,
+                                       static_cast<const T *>(logits), rows, E, ld, temperature, row_mask, t_idx, t_logit, t_lse, K, d_loss, accumulate,
+                                       static_cast<T *>(d_logits), ld_d);
+                });
             });
         });
     });

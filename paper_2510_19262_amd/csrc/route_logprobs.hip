@@ -33,7 +33,7 @@ __global__ __launch_bounds__(256) void route_logprobs_kernel(const T *__restrict
         const float log_total = log2_of(soft.total);
         if (there && q == 0) {
             if (lse) lse[row] = counts ? fmaf(soft.largest, inv_tau, kLn2 * log_total) : 0.0f;
-            if (entropy) entropy[row] = counts ? kLn2 * (log_total - dot / soft.total) : 0.0f;
+            if (entropy) entropy[row] = counts ? kLn2 * (log_total - dot * inverse(soft.total)) : 0.0f;
         }
         if (there) {
             for (int j = q; j < k; j += LANES) {
@@ -114,7 +114,7 @@ __global__ __launch_bounds__(256) void route_logprobs_backward_kernel(const T *_
             sum = row_sum<LANES>(sum);
         }
         const float pull = sum - (d_lse && live ? d_lse[row] : 0.0f);
-        const float scale = 1.0f / soft.total;
+        const float scale = inverse(soft.total);
         if (d_entropy) {
             const float mean = row_dot<LANES, VPL>(y, e) * scale;
             const float gh = live ? kLn2 * d_entropy[row] : 0.0f;

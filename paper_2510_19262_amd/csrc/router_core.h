@@ -5,6 +5,8 @@
 
 #include "topk_core.h"
 
+#include <type_traits>
+
 namespace rs {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -121,6 +123,7 @@ __device__ __forceinline__ void row_store(T *__restrict__ row, int E, int q, boo
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 __device__ __forceinline__ float pow2(float y) { return __builtin_amdgcn_exp2f(y); }
 __device__ __forceinline__ float log2_of(float v) { return __builtin_amdgcn_logf(v); }       // of normal numbers, to one step
+__device__ __forceinline__ float inverse(float v) { return __builtin_amdgcn_rcpf(v); }        // likewise: a tenth of a division's instructions
 
 // Softmax of a row: x holds the logits on entry and y on return, e the powers.
 struct RowSoft {
@@ -281,9 +284,14 @@ inline int by_shape(int E, bool fours, F f)
     if (E <= 512) return f(Shape<32, 16, true>());
     return f(Shape<64, 16, true>());
 }
-// lists of at most kMaxListed entries, and of at most E, over the lanes of a row
-template <typename S>
-constexpr int list_regs() { return S::VPL < kMaxListed / S::LANES ? S::VPL : kMaxListed / S::LANES; }
+// f(how many of `count` <= kMaxListed entries of a list a lane holds, at most): 1 where they fit, or as many as the longest list takes (of E entries at most)
+template <typename S, typename F>
+inline int by_entries(int count, F f)
+{
+    constexpr int most = S::VPL < kMaxListed / S::LANES ? S::VPL : kMaxListed / S::LANES;
+    if (most == 1 || count <= S::LANES) return f(std::integral_constant<int, 1>());
+    return f(std::integral_constant<int, most>());
+}
 
 // f(T()) for the type that dtype names
 template <typename F>
