@@ -305,7 +305,7 @@ int railsched_port_round_robin(const int64_t *chunk_off, const uint8_t *rail, in
  *             A logit may be -infinity: that expert is out for this row (probability 0).  A row with NaN or
  *             +infinity makes NaN of the floating outputs it enters and of no others.
  *   row_mask  [rows] uint8, NULL = all rows count.  A row whose entry is 0 (padding) does not count, and neither does a
- *             row whose logits are all -infinity: its logits (if masked) are not read, its picks are not counted, its
+ *             row whose logits are all -infinity: whatever a masked row holds enters nothing, its picks are not counted, its
  *             floating outputs and its gradient are 0, its alternatives -1.
  *   temperature  tau, within 2^-100 .. 2^100: z = logits / tau, p = softmax(z) over the row, lse = log sum exp z.
  *   d_logits  the gradient, type `dtype`, row r at d_logits + r*ld_d, ld_d >= E; not the same memory as logits.  Places

@@ -100,18 +100,21 @@ __global__ __launch_bounds__(256) void route_balance_kernel(const T *__restrict_
         for (int j = 0; j < VPL; ++j) acc[j] = 0.0f;
         unsigned here = 0;
         for (int64_t w0 = lo; w0 < hi; w0 += ROWS_PER_BLOCK) {
-            const int64_t row = w0 + slot;
-            const bool live = row < hi && (!row_mask || row_mask[row] != 0);
+            const RowAt at_row = row_at(slot, hi - w0, row_mask, w0);
+            const int32_t *__restrict__ chosen = topk_idx + w0 * k + at_row.slot * k;
+            const int pick = chosen[q < k ? q : 0];                  // a lane's first pick is fetched with the row
             float t[VPL], e[VPL];
-            row_values<T, LANES, VPL, VEC>(logits + row * ld, live, E, q, t);
+            row_values<T, LANES, VPL, VEC>(row_of(logits + w0 * ld, at_row.slot, ld), E, q, t);
             const RowSoft soft = row_softmax<LANES, VPL>(t, e, kLog2e);
-            if (soft.total != 0.0f) {
-                const float scale = inverse(soft.total);
+            const bool use = at_row.live && soft.total != 0.0f;
+            const float scale = inverse(soft.total);
 #pragma unroll
-                for (int j = 0; j < VPL; ++j) acc[j] += e[j] * scale;
+            for (int j = 0; j < VPL; ++j) acc[j] += use ? e[j] * scale : 0.0f;
+            if (use) {
                 here += q == 0;
-                for (int j = q; j < k; j += LANES) {
-                    const int at = topk_idx[row * k + j];
+                if (q < k && pick >= 0 && pick < E) atomicAdd(&picks[pick], 1u);
+                for (int j = q + LANES; j < k; j += LANES) {
+                    const int at = chosen[j];
                     if (at >= 0 && at < E) atomicAdd(&picks[at], 1u);
                 }
             }
@@ -245,13 +248,11 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
             a[j] = i < E ? weight[i] : 0.0f;
         }
         for (int64_t w0 = lo; w0 < hi; w0 += ROWS_PER_BLOCK) {
-            const int64_t row = w0 + slot;
-            const bool there = row < hi;
-            const bool live = there && (!row_mask || row_mask[row] != 0);
+            const RowAt at_row = row_at(slot, hi - w0, row_mask, w0);
             float t[VPL], e[VPL];
-            row_values<T, LANES, VPL, VEC>(logits + row * ld, live, E, q, t);
+            row_values<T, LANES, VPL, VEC>(row_of(logits + w0 * ld, at_row.slot, ld), E, q, t);
             const RowSoft soft = row_softmax<LANES, VPL>(t, e, kLog2e);
-            const bool counts_here = soft.total != 0.0f;
+            const bool counts_here = at_row.live && soft.total != 0.0f;
             const float scale = inverse(soft.total);
             float ap = 0.0f;
 #pragma unroll
@@ -262,7 +263,7 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
             ap = row_sum<LANES>(ap);
 #pragma unroll
             for (int j = 0; j < VPL; ++j) t[j] = counts_here ? e[j] * (a[j] - ap) : 0.0f;
-            if (there && (counts_here || !add)) row_store<T, LANES, VPL, VEC>(d_logits + row * ld_d, E, q, add != 0, t);
+            if (at_row.there && (counts_here || !add)) row_store<T, LANES, VPL, VEC>(d_logits + (w0 + slot) * ld_d, E, q, add != 0, t);
         }
         __syncthreads();
     }

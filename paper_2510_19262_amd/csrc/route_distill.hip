@@ -54,29 +54,38 @@ struct Distilled {
     bool listed;                 // whether the row has entries at all
 };
 
+// The row `at_row` of the rows from `first` on.
 template <typename T, int LANES, int VPL, bool VEC, int NK>
-__device__ __forceinline__ void distill_row(const T *__restrict__ logits, int64_t row, bool live, int E, int64_t ld, float inv_tau,
+__device__ __forceinline__ void distill_row(const T *__restrict__ logits, int64_t first, const RowAt &at_row, int E, int64_t ld, float inv_tau,
                                             const int32_t *__restrict__ t_idx, const float *__restrict__ t_logit,
                                             const float *__restrict__ t_lse, int K, int q0, float *mine, Distilled<LANES, VPL, NK> &o)
 {
-    const T *__restrict__ from = logits + row * ld;
-    row_values<T, LANES, VPL, VEC>(from, live, E, q0, o.y);
+    const T *__restrict__ from = row_of(logits + first * ld, at_row.slot, ld);
+    const int entry0 = at_row.slot * K;
+    t_idx += first * K;
+    t_logit += first * K;
     float tl[NK], xl[NK];
-    float best = -INFINITY;
-    bool any = false;
 #pragma unroll
     for (int r = 0; r < NK; ++r) {
         o.at[r] = -1;
         tl[r] = -INFINITY;
-        xl[r] = 0.0f;
         if (LANES * r < K) {                             // the same for every lane: entries that no lane has cost nothing
             const int j = q0 + LANES * r;
-            if (live && j < K) {
-                o.at[r] = t_idx[row * K + j];
-                tl[r] = t_logit[row * K + j];
-            }
+            o.at[r] = t_idx[entry0 + (j < K ? j : 0)];
+            tl[r] = t_logit[entry0 + (j < K ? j : 0)];
+            if (j >= K) o.at[r] = -1;
+        }
+    }
+    const float teacher = t_lse ? t_lse[first + at_row.slot] : 0.0f;
+    row_values<T, LANES, VPL, VEC>(from, E, q0, o.y);
+    float best = -INFINITY;
+    bool any = false;
+#pragma unroll
+    for (int r = 0; r < NK; ++r) {
+        xl[r] = 0.0f;
+        if (LANES * r < K) {
             if (o.at[r] < 0 || o.at[r] >= E || tl[r] == -INFINITY) { o.at[r] = -1; tl[r] = -INFINITY; }
-            if (o.at[r] >= 0) xl[r] = (float)from[o.at[r]];
+            xl[r] = (float)from[o.at[r] < 0 ? 0 : o.at[r]];
             best = fmaxf(best, tl[r]);
             any |= o.at[r] >= 0;
         }
@@ -92,7 +101,7 @@ __device__ __forceinline__ void distill_row(const T *__restrict__ logits, int64_
     // q, and the logarithm of the teacher's total mass
     float log_mass;
     if (t_lse) {
-        log_mass = live ? t_lse[row] : 0.0f;
+        log_mass = teacher;
 #pragma unroll
         for (int r = 0; r < NK; ++r) o.q[r] = LANES * r < K && o.at[r] >= 0 ? pow2(kLog2e * fmaf(tl[r], inv_tau, -log_mass)) : 0.0f;
     } else {
@@ -143,12 +152,10 @@ __global__ __launch_bounds__(256) void route_distill_kernel(const T *__restrict_
     float *mine = lds + threadIdx.x / LANES * (LANES * VPL);
     const float inv_tau = 1.0f / tau;
     const int64_t stride = (int64_t)gridDim.x * ROWS_PER_BLOCK;
-    for (int64_t w0 = (int64_t)blockIdx.x * ROWS_PER_BLOCK; w0 < rows; w0 += stride) {
-        const int64_t row = w0 + threadIdx.x / LANES;
-        const bool there = row < rows;
-        const bool live = there && (!row_mask || row_mask[row] != 0);
+    for (int64_t first = (int64_t)blockIdx.x * ROWS_PER_BLOCK; first < rows; first += stride) {
+        const RowAt at_row = row_at(threadIdx.x / LANES, rows - first, row_mask, first);
         Distilled<LANES, VPL, NK> o;
-        distill_row<T, LANES, VPL, VEC, NK>(logits, row, live, E, ld, inv_tau, t_idx, t_logit, t_lse, K, q0, mine, o);
+        distill_row<T, LANES, VPL, VEC, NK>(logits, first, at_row, E, ld, inv_tau, t_idx, t_logit, t_lse, K, q0, mine, o);
         float terms = 0.0f, twice = 0.0f;
 #pragma unroll
         for (int r = 0; r < NK; ++r) {
@@ -168,7 +175,7 @@ __global__ __launch_bounds__(256) void route_distill_kernel(const T *__restrict_
         } else {
             sum += o.rest_p + (o.mass - 1.0f);
         }
-        if (there && q0 == 0) loss[row] = o.soft.total != 0.0f && o.listed ? tau * tau * sum : 0.0f;
+        if (at_row.there && q0 == 0) loss[first + threadIdx.x / LANES] = at_row.live && o.soft.total != 0.0f && o.listed ? tau * tau * sum : 0.0f;
         lds_order();
     }
 }
@@ -186,19 +193,18 @@ __global__ __launch_bounds__(256) void route_distill_backward_kernel(const T *__
     float *mine = lds + threadIdx.x / LANES * (LANES * VPL);
     const float inv_tau = 1.0f / tau;
     const int64_t stride = (int64_t)gridDim.x * ROWS_PER_BLOCK;
-    for (int64_t w0 = (int64_t)blockIdx.x * ROWS_PER_BLOCK; w0 < rows; w0 += stride) {
-        const int64_t row = w0 + threadIdx.x / LANES;
-        const bool there = row < rows;
-        const bool live = there && (!row_mask || row_mask[row] != 0);
+    for (int64_t first = (int64_t)blockIdx.x * ROWS_PER_BLOCK; first < rows; first += stride) {
+        const RowAt at_row = row_at(threadIdx.x / LANES, rows - first, row_mask, first);
         Distilled<LANES, VPL, NK> o;
-        distill_row<T, LANES, VPL, VEC, NK>(logits, row, live, E, ld, inv_tau, t_idx, t_logit, t_lse, K, q0, mine, o);
-        const bool counts = o.soft.total != 0.0f;
+        distill_row<T, LANES, VPL, VEC, NK>(logits, first, at_row, E, ld, inv_tau, t_idx, t_logit, t_lse, K, q0, mine, o);
+        const bool counts = at_row.live && o.soft.total != 0.0f;
+        const float along = d_loss[first + at_row.slot];
         lds_order();
         lds_put<LANES, NK>(mine, q0, K, o.at, o.again, o.q);
         float listed[VPL];
         lds_values<LANES, VPL, VEC>(mine, q0, listed);
         lds_order();
-        const float unit = live && o.listed ? tau * d_loss[row] : 0.0f;
+        const float unit = tau * along;
         const float scale = inverse(o.soft.total);
         const float inside = (o.mass + o.rest_q) * scale;
         // Q + q_r - q_r / p_r is (p_r - q_r) / p_r where sum q + q_r is 1
@@ -208,7 +214,7 @@ __global__ __launch_bounds__(256) void route_distill_backward_kernel(const T *__
             const float g = listed[j] < 0.0f ? o.e[j] * outside : o.e[j] * inside - listed[j];
             o.y[j] = counts && o.listed ? unit * g : 0.0f;
         }
-        if (there && (counts || !add)) row_store<T, LANES, VPL, VEC>(d_logits + row * ld_d, E, q0, add != 0, o.y);
+        if (at_row.there && (counts || !add)) row_store<T, LANES, VPL, VEC>(d_logits + (first + threadIdx.x / LANES) * ld_d, E, q0, add != 0, o.y);
     }
 }
 

@@ -7,7 +7,44 @@
 
 namespace rs {
 
-template <typename T, int LANES, int VPL, bool VEC>
+// How the most likely experts of a row are found: not at all, one round over the row each, or by the lists of stage 1's kernels.
+enum { ALT_NONE = 0, ALT_ROUNDS = 1, ALT_LISTS = 2 };
+
+template <int LANES>
+__device__ __forceinline__ int row_min(int v)
+{
+    if constexpr (LANES <= 16) v = group_min<LANES>(v);
+    else {
+        v = group_min<16>(v);
+        v = min(v, xlane<16>(v));
+        if constexpr (LANES == 64) v = min(v, xlane<32>(v));
+    }
+    return v;
+}
+
+// The m largest logits of the row, one round each: emit(sel, expert) in every lane of the row, INT_MAX once only -infinity is left (and NaN, which is never
+// taken).  The winners are taken out of x.
+template <int LANES, int VPL, bool VEC, typename F>
+__device__ __forceinline__ void row_rounds(float (&x)[VPL], int m, int q, F emit)
+{
+    for (int sel = 0; sel < m; ++sel) {
+        float best = x[0];
+#pragma unroll
+        for (int j = 1; j < VPL; ++j) best = fmaxf(best, x[j]);
+        best = row_max<LANES>(best);
+        int slot = VPL;
+#pragma unroll
+        for (int j = VPL - 1; j >= 0; --j) slot = x[j] == best ? j : slot;
+        const int mine = slot < VPL && best > -INFINITY ? slot_index<LANES, VPL, VEC>(q, slot) : INT_MAX;
+        const int winner = row_min<LANES>(mine);
+        const int gone = winner == mine ? slot : VPL;
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) x[j] = j == gone ? -INFINITY : x[j];
+        emit(sel, winner);
+    }
+}
+
+template <typename T, int LANES, int VPL, bool VEC, int ALT, int L>
 __global__ __launch_bounds__(256) void route_logprobs_kernel(const T *__restrict__ logits, int64_t rows, int E, int64_t ld, float inv_tau,
                                                              const uint8_t *__restrict__ row_mask, const int32_t *__restrict__ topk_idx,
                                                              int k, int m, float *__restrict__ logp, float *__restrict__ lse,
@@ -16,47 +53,70 @@ __global__ __launch_bounds__(256) void route_logprobs_kernel(const T *__restrict
 {
     constexpr int ROWS_PER_BLOCK = 256 / LANES;
     const int q = threadIdx.x % LANES;
+    const float c = inv_tau * kLog2e;
     const int64_t stride = (int64_t)gridDim.x * ROWS_PER_BLOCK;
-    for (int64_t w0 = (int64_t)blockIdx.x * ROWS_PER_BLOCK; w0 < rows; w0 += stride) {          // the same for every lane
-        const int64_t row = w0 + threadIdx.x / LANES;
-        const bool there = row < rows;
-        const bool live = there && (!row_mask || row_mask[row] != 0);
-        const T *__restrict__ from = logits + row * ld;
-        float raw[VPL], y[VPL], e[VPL];
-        row_values<T, LANES, VPL, VEC>(from, live, E, q, raw);
-#pragma unroll
-        for (int j = 0; j < VPL; ++j) y[j] = raw[j];
-        const float c = inv_tau * kLog2e;
-        const RowSoft soft = row_softmax<LANES, VPL>(y, e, c);
-        const float dot = row_dot<LANES, VPL>(y, e);
-        const bool counts = soft.total != 0.0f;
+    for (int64_t first = (int64_t)blockIdx.x * ROWS_PER_BLOCK; first < rows; first += stride) {          // the same for every lane
+        const RowAt at_row = row_at(threadIdx.x / LANES, rows - first, row_mask, first);
+        const bool there = at_row.there;
+        const int64_t row = first + threadIdx.x / LANES;
+        const T *__restrict__ from = row_of(logits + first * ld, at_row.slot, ld);
+        const int32_t *__restrict__ ask = topk_idx + first * k + at_row.slot * k;
+        int pick = -1;
+        if (k > 0) {                                     // a lane's first pick is fetched with the row
+            pick = ask[q < k ? q : 0];
+            if (pick >= E) pick = -1;
+        }
+        float x[VPL], dot;
+        row_values<T, LANES, VPL, VEC>(from, E, q, x);
+        const float picked = (float)from[pick < 0 ? 0 : pick];
+        const RowSoft soft = row_sums<LANES, VPL>(x, c, dot);
+        const bool counts = at_row.live && soft.total != 0.0f;
         const float log_total = log2_of(soft.total);
         if (there && q == 0) {
             if (lse) lse[row] = counts ? fmaf(soft.largest, inv_tau, kLn2 * log_total) : 0.0f;
             if (entropy) entropy[row] = counts ? kLn2 * (log_total - dot * inverse(soft.total)) : 0.0f;
         }
+        if (there && q < k) logp[row * k + q] = counts && pick >= 0 ? kLn2 * (soft.y(picked, c) - log_total) : 0.0f;
         if (there) {
-            for (int j = q; j < k; j += LANES) {
-                const int at = topk_idx[row * k + j];
+            for (int j = q + LANES; j < k; j += LANES) {
+                const int at = ask[j];
                 const bool good = counts && at >= 0 && at < E;
                 logp[row * k + j] = good ? kLn2 * (soft.y((float)from[at], c) - log_total) : 0.0f;
             }
         }
-        for (int sel = 0; sel < m; ++sel) {
-            float best = -INFINITY;
-            int at = INT_MAX;
+        if constexpr (ALT != ALT_NONE) {
+            auto put = [&](int sel, int at) {            // an alternative: its logit once more, from the cache
+                const float v = at < E ? (float)from[at] : -INFINITY;
+                const bool good = counts && v != -INFINITY;
+                alt_idx[row * m + sel] = good ? at : -1;
+                alt_logp[row * m + sel] = good ? kLn2 * (soft.y(v, c) - log_total) : counts ? -INFINITY : 0.0f;
+            };
+            auto each = [&](int sel, int at) {
+                if (there && q == sel % LANES) put(sel, at);
+            };
+            if constexpr (ALT == ALT_ROUNDS) {
+                row_rounds<LANES, VPL, VEC>(x, m, q, each);
+            } else {
+                constexpr int KM = 8;
+                constexpr unsigned MASK = (unsigned)(LANES * VPL) - 1u;
+                float4 v[VPL / 4];
 #pragma unroll
-            for (int j = 0; j < VPL; ++j) {
-                const bool better = raw[j] > best;
-                best = better ? raw[j] : best;
-                at = better ? slot_index<LANES, VPL, VEC>(q, j) : at;
-            }
-            group_argmax<LANES>(best, at);
+                for (int i = 0; i < VPL / 4; ++i) v[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+                int own[L];
+                unsigned bits, u[KM];
+                lane_best<LANES, VPL, L, false>(v, E, q, own, bits);
+                const bool bad = row_best<LANES, VPL, L, KM>(own, bits, m, u);
+                if (__ballot(there && bad) == 0ull) {
 #pragma unroll
-            for (int j = 0; j < VPL; ++j) raw[j] = slot_index<LANES, VPL, VEC>(q, j) == at ? -INFINITY : raw[j];
-            if (there && q == sel % LANES) {
-                alt_idx[row * m + sel] = at < E ? at : -1;
-                alt_logp[row * m + sel] = !counts ? 0.0f : at < E ? kLn2 * (soft.y(best, c) - log_total) : -INFINITY;
+                    for (int r = 0; r < (KM + LANES - 1) / LANES; ++r) {     // alternatives q, q + LANES, ... of this lane
+                        unsigned sel = 0;
+#pragma unroll
+                        for (int j = r * LANES; j < KM && j < (r + 1) * LANES; ++j) sel = j == q + r * LANES ? u[j] : sel;
+                        if (there && q + r * LANES < m) put(q + r * LANES, (int)key_index<MASK>(sel));
+                    }
+                } else {
+                    row_rounds<LANES, VPL, VEC>(x, m, q, each);
+                }
             }
         }
     }
@@ -77,35 +137,36 @@ __global__ __launch_bounds__(256) void route_logprobs_backward_kernel(const T *_
     const int q = threadIdx.x % LANES;
     float *mine = lds + threadIdx.x / LANES * (LANES * VPL);
     const int64_t stride = (int64_t)gridDim.x * ROWS_PER_BLOCK;
-    for (int64_t w0 = (int64_t)blockIdx.x * ROWS_PER_BLOCK; w0 < rows; w0 += stride) {
-        const int64_t row = w0 + threadIdx.x / LANES;
-        const bool there = row < rows;
-        const bool live = there && (!row_mask || row_mask[row] != 0);
+    for (int64_t first = (int64_t)blockIdx.x * ROWS_PER_BLOCK; first < rows; first += stride) {
+        const RowAt at_row = row_at(threadIdx.x / LANES, rows - first, row_mask, first);
         float y[VPL], e[VPL];
-        row_values<T, LANES, VPL, VEC>(logits + row * ld, live, E, q, y);
-        const RowSoft soft = row_softmax<LANES, VPL>(y, e, inv_tau * kLog2e);
-        const bool counts = soft.total != 0.0f;
+        row_values<T, LANES, VPL, VEC>(row_of(logits + first * ld, at_row.slot, ld), E, q, y);
+        const int64_t entry0 = first * k + at_row.slot * k;
+        const float along = d_lse ? d_lse[first + at_row.slot] : 0.0f;
+        const float spread = d_entropy ? kLn2 * d_entropy[first + at_row.slot] : 0.0f;
 
         float dx[VPL], sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < VPL; ++j) dx[j] = 0.0f;
         if (d_logp) {
-            for (int first = 0; first < k; first += LANES * NK) {            // NK entries a lane at a time
+            for (int j0 = 0; j0 < k; j0 += LANES * NK) {             // NK entries a lane at a time
                 int at[NK];
                 bool again[NK];
                 float g[NK], part[VPL];
 #pragma unroll
                 for (int r = 0; r < NK; ++r) {
-                    const int j = first + q + LANES * r;
-                    at[r] = live && j < k ? topk_idx[row * k + j] : -1;
-                    if (at[r] >= E) at[r] = -1;
-                    g[r] = at[r] >= 0 ? d_logp[row * k + j] : 0.0f;
+                    const int j = j0 + q + LANES * r;
+                    const int64_t entry = entry0 + (j < k ? j : 0);
+                    at[r] = topk_idx[entry];
+                    g[r] = d_logp[entry];
+                    if (j >= k || at[r] >= E) at[r] = -1;
+                    if (at[r] < 0) g[r] = 0.0f;
                     sum += g[r];
                 }
                 lds_fill<LANES, VPL, VEC>(mine, q, 0.0f);
                 lds_order();
-                lds_mark<LANES, NK>(mine, q, k - first, at, again);
-                lds_put<LANES, NK>(mine, q, k - first, at, again, g);
+                lds_mark<LANES, NK>(mine, q, k - j0, at, again);
+                lds_put<LANES, NK>(mine, q, k - j0, at, again, g);
                 lds_values<LANES, VPL, VEC>(mine, q, part);
                 lds_order();
 #pragma unroll
@@ -113,28 +174,28 @@ __global__ __launch_bounds__(256) void route_logprobs_backward_kernel(const T *_
             }
             sum = row_sum<LANES>(sum);
         }
-        const float pull = sum - (d_lse && live ? d_lse[row] : 0.0f);
-        const float scale = inverse(soft.total);
+        const RowSoft soft = row_softmax<LANES, VPL>(y, e, inv_tau * kLog2e);
+        const bool counts = at_row.live && soft.total != 0.0f;
+        const float scale = inverse(soft.total), pull = sum - along;
         if (d_entropy) {
             const float mean = row_dot<LANES, VPL>(y, e) * scale;
-            const float gh = live ? kLn2 * d_entropy[row] : 0.0f;
 #pragma unroll
-            for (int j = 0; j < VPL; ++j) dx[j] -= e[j] * scale * (pull + gh * (fmaxf(y[j], -1e30f) - mean));
+            for (int j = 0; j < VPL; ++j) dx[j] -= e[j] * scale * (pull + spread * (fmaxf(y[j], -1e30f) - mean));
         } else {
 #pragma unroll
             for (int j = 0; j < VPL; ++j) dx[j] -= e[j] * scale * pull;
         }
 #pragma unroll
         for (int j = 0; j < VPL; ++j) dx[j] = counts ? dx[j] * inv_tau : 0.0f;
-        if (there && (counts || !add)) row_store<T, LANES, VPL, VEC>(d_logits + row * ld_d, E, q, add != 0, dx);
+        if (at_row.there && (counts || !add)) row_store<T, LANES, VPL, VEC>(d_logits + (first + threadIdx.x / LANES) * ld_d, E, q, add != 0, dx);
     }
 }
 
-template <typename T, int LANES, int VPL, bool VEC, typename... A>
+template <typename T, int LANES, int VPL, bool VEC, int ALT, int L, typename... A>
 static int launch_logprobs(const T *logits, int64_t rows, hipStream_t st, A... rest)
 {
     const int64_t blocks = (rows + 256 / LANES - 1) / (256 / LANES);
-    hipLaunchKernelGGL((route_logprobs_kernel<T, LANES, VPL, VEC>), dim3((unsigned)(blocks < (1 << 22) ? blocks : 1 << 22)), dim3(256), 0, st, logits, rows,
+    hipLaunchKernelGGL((route_logprobs_kernel<T, LANES, VPL, VEC, ALT, L>), dim3((unsigned)(blocks < (1 << 22) ? blocks : 1 << 22)), dim3(256), 0, st, logits, rows,
                        rest...);
     return launch_status();
 }
@@ -162,10 +223,24 @@ extern "C" int railsched_route_logprobs(const void *logits, int32_t dtype, int64
     hipStream_t st = static_cast<hipStream_t>(stream);
     return by_dtype(dtype, [&](auto t) {
         using T = decltype(t);
-        return by_shape(E, in_fours<T>(logits, E, ld), [&](auto s) {
+        auto go = [&](auto s, auto alt, auto length) {
             using S = decltype(s);
-            return launch_logprobs<T, S::LANES, S::VPL, S::VEC>(static_cast<const T *>(logits), rows, st, E, ld, 1.0f / temperature, row_mask, topk_idx, k,
-                                                                m, logp, lse, entropy, alt_idx, alt_logp);
+            return launch_logprobs<T, S::LANES, S::VPL, S::VEC, decltype(alt)::value, decltype(length)::value>(
+                static_cast<const T *>(logits), rows, st, E, ld, 1.0f / temperature, row_mask, topk_idx, k, m, logp, lse, entropy, alt_idx, alt_logp);
+        };
+        const bool fours = in_fours<T>(logits, E, ld);
+        // up to eight alternatives of rows of more than 32 logits come from stage 1's lists, in the shapes and list lengths that it uses
+        if (fours && E > 32 && m > 0 && m <= 8) {
+            constexpr std::integral_constant<int, ALT_LISTS> lists;
+            if (E <= 64) return go(Shape<4, 16, true>(), lists, std::integral_constant<int, 8>());
+            if (E <= 128) return go(Shape<8, 16, true>(), lists, std::integral_constant<int, 6>());
+            if (E <= 256) return go(Shape<16, 16, true>(), lists, std::integral_constant<int, 5>());
+            if (E <= 512) return go(Shape<16, 32, true>(), lists, std::integral_constant<int, 5>());
+            return go(Shape<16, 64, true>(), lists, std::integral_constant<int, 5>());
+        }
+        return by_shape(E, fours, [&](auto s) {
+            if (m > 0) return go(s, std::integral_constant<int, ALT_ROUNDS>(), std::integral_constant<int, 0>());
+            return go(s, std::integral_constant<int, ALT_NONE>(), std::integral_constant<int, 0>());
         });
     });
 }

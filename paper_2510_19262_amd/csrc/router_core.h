@@ -44,16 +44,22 @@ __device__ __forceinline__ void store4(T *p, const float (&v)[4])
     }
 }
 
-// ---- sums and maxima over the LANES lanes of a row, in all of them
+// ---- sums and maxima over the LANES lanes of a row, in all of them.  Inside 16 lanes the partner's value is an operand of the addition itself.
+template <int OFF>
+__device__ __forceinline__ float partner(float v)
+{
+    if constexpr (OFF <= 8) return __int_as_float(from_partner<OFF>(__float_as_int(v)));
+    else return xlane<OFF>(v);
+}
 template <int LANES, typename F>
 __device__ __forceinline__ float row_reduce(float v, F op)
 {
-    if constexpr (LANES >= 2) v = op(v, xlane<1>(v));
-    if constexpr (LANES >= 4) v = op(v, xlane<2>(v));
-    if constexpr (LANES >= 8) v = op(v, xlane<4>(v));
-    if constexpr (LANES >= 16) v = op(v, xlane<8>(v));
-    if constexpr (LANES >= 32) v = op(v, xlane<16>(v));
-    if constexpr (LANES >= 64) v = op(v, xlane<32>(v));
+    if constexpr (LANES >= 2) v = op(v, partner<1>(v));
+    if constexpr (LANES >= 4) v = op(v, partner<2>(v));
+    if constexpr (LANES >= 8) v = op(v, partner<4>(v));
+    if constexpr (LANES >= 16) v = op(v, partner<8>(v));
+    if constexpr (LANES >= 32) v = op(v, partner<16>(v));
+    if constexpr (LANES >= 64) v = op(v, partner<32>(v));
     return v;
 }
 template <int LANES>
@@ -70,25 +76,50 @@ __device__ __forceinline__ bool row_any(bool v)
     else return ((all >> (threadIdx.x & 63u & ~(unsigned)(LANES - 1))) & ((1ull << LANES) - 1ull)) != 0ull;
 }
 
-// This lane's values of a row as fp32; places that do not exist (and whole rows that are not live, which are not read) are -infinity.
+// ---- which row the lanes are at.  A workgroup has the rows first, first + 1, ... in hand, one to LANES lanes, of which `left` exist.  Lanes without a row, and
+// lanes whose row is masked, follow the workgroup's first row instead: their loads need no branch (a load under a condition is waited for before
+// the next one is made), read what is read anyway, and what comes of them is not used.
+struct RowAt {
+    int slot;       // the row followed, from the first one
+    bool there;     // a row of its own
+    bool live;      // that is not masked
+};
+__device__ __forceinline__ RowAt row_at(int slot, int64_t left, const uint8_t *__restrict__ row_mask, int64_t first)
+{
+    RowAt r;
+    r.there = slot < left;
+    r.slot = r.there ? slot : 0;
+    r.live = r.there;
+    if (row_mask) {
+        r.live = r.there && row_mask[first + r.slot] != 0;
+        r.slot = r.live ? r.slot : 0;
+    }
+    return r;
+}
+// row `slot` of rows `ld` apart (both below 2^32)
+template <typename T>
+__device__ __forceinline__ T *row_of(T *first, int slot, int64_t ld) { return first + (uint64_t)(uint32_t)slot * (uint32_t)ld; }
+
+// This lane's values of a row as fp32; places behind the row are -infinity.
 // VEC: places of four consecutive experts, interleaved over the lanes, as slot_index() numbers them.
 template <typename T, int LANES, int VPL, bool VEC>
-__device__ __forceinline__ void row_values(const T *__restrict__ row, bool live, int E, int q, float (&x)[VPL])
+__device__ __forceinline__ void row_values(const T *__restrict__ row, int E, int q, float (&x)[VPL])
 {
     if constexpr (VEC) {
 #pragma unroll
         for (int c = 0; c < VPL / 4; ++c) {
-            float v[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            float v[4];
             const int e0 = 4 * (q + LANES * c);
-            if (live && e0 < E) load4(row + e0, v);
+            load4(row + (e0 < E ? e0 : 0), v);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[4 * c + i] = v[i];
+            for (int i = 0; i < 4; ++i) x[4 * c + i] = e0 < E ? v[i] : -INFINITY;
         }
     } else {
 #pragma unroll
         for (int j = 0; j < VPL; ++j) {
             const int e = q + LANES * j;
-            x[j] = (live && e < E) ? (float)row[e] : -INFINITY;
+            const float v = (float)row[e < E ? e : 0];
+            x[j] = e < E ? v : -INFINITY;
         }
     }
 }
@@ -148,6 +179,28 @@ __device__ __forceinline__ RowSoft row_softmax(float (&x)[VPL], float (&e)[VPL],
         s += e[j];
     }
     r.total = row_sum<LANES>(s);
+    return r;
+}
+
+// The same without the powers: the logits stay as they are, and dot is the sum of 2^y y.
+template <int LANES, int VPL>
+__device__ __forceinline__ RowSoft row_sums(const float (&x)[VPL], float c, float &dot)
+{
+    RowSoft r;
+    float m = x[0];
+#pragma unroll
+    for (int j = 1; j < VPL; ++j) m = fmaxf(m, x[j]);
+    m = row_max<LANES>(m);
+    r.largest = m == -INFINITY ? 0.0f : m;
+    float s = 0.0f, d = 0.0f;
+#pragma unroll
+    for (int j = 0; j < VPL; ++j) {
+        const float y = r.y(x[j], c), e = pow2(y);
+        s += e;
+        d = fmaf(e, fmaxf(y, -1e30f), d);
+    }
+    r.total = row_sum<LANES>(s);
+    dot = row_sum<LANES>(d);
     return r;
 }
 
