@@ -151,33 +151,32 @@ __global__ __launch_bounds__(256) void route_distill_kernel(const T *__restrict_
     const int q0 = threadIdx.x % LANES;
     float *mine = lds + threadIdx.x / LANES * (LANES * VPL);
     const float inv_tau = 1.0f / tau;
-    const int64_t stride = (int64_t)gridDim.x * ROWS_PER_BLOCK;
-    for (int64_t first = (int64_t)blockIdx.x * ROWS_PER_BLOCK; first < rows; first += stride) {
-        const RowAt at_row = row_at(threadIdx.x / LANES, rows - first, row_mask, first);
-        Distilled<LANES, VPL, NK> o;
-        distill_row<T, LANES, VPL, VEC, NK>(logits, first, at_row, E, ld, inv_tau, t_idx, t_logit, t_lse, K, q0, mine, o);
-        float terms = 0.0f, twice = 0.0f;
+    const int64_t first = first_row(ROWS_PER_BLOCK);
+    if (first >= rows) return;
+    const RowAt at_row = row_at(threadIdx.x / LANES, rows - first, row_mask, first);
+    Distilled<LANES, VPL, NK> o;
+    distill_row<T, LANES, VPL, VEC, NK>(logits, first, at_row, E, ld, inv_tau, t_idx, t_logit, t_lse, K, q0, mine, o);
+    float terms = 0.0f, twice = 0.0f;
 #pragma unroll
-        for (int r = 0; r < NK; ++r) {
-            if (LANES * r < K && o.at[r] >= 0) {
-                // q (e^d - 1 - d) where e^d does not carry it off, and p alone where q has vanished
-                terms += o.q[r] == 0.0f ? o.p[r] : o.d[r] < 1.0f ? o.q[r] * exp_above(o.d[r]) : o.p[r] - o.q[r] - o.q[r] * o.d[r];
-                if (o.again[r]) twice += o.p[r];
-            }
+    for (int r = 0; r < NK; ++r) {
+        if (LANES * r < K && o.at[r] >= 0) {
+            // q (e^d - 1 - d) where e^d does not carry it off, and p alone where q has vanished
+            terms += o.q[r] == 0.0f ? o.p[r] : o.d[r] < 1.0f ? o.q[r] * exp_above(o.d[r]) : o.p[r] - o.q[r] - o.q[r] * o.d[r];
+            if (o.again[r]) twice += o.p[r];
         }
-        terms = row_sum<LANES>(terms);
-        if (__ballot(twice != 0.0f) != 0ull) twice = row_sum<LANES>(twice);
-        // sum q + q_r - (sum of p over the entries and outside): p of an expert listed twice is in its terms twice
-        float sum = terms - twice;
-        if (t_lse && o.rest_q > 0.0f) {
-            const float apart = o.gap / o.rest_q;                        // p_r / q_r - 1
-            sum += o.rest_q * above_log(apart);
-        } else {
-            sum += o.rest_p + (o.mass - 1.0f);
-        }
-        if (at_row.there && q0 == 0) loss[first + threadIdx.x / LANES] = at_row.live && o.soft.total != 0.0f && o.listed ? tau * tau * sum : 0.0f;
-        lds_order();
     }
+    terms = row_sum<LANES>(terms);
+    if (__ballot(twice != 0.0f) != 0ull) twice = row_sum<LANES>(twice);
+    // sum q + q_r - (sum of p over the entries and outside): p of an expert listed twice is in its terms twice
+    float sum = terms - twice;
+    if (t_lse && o.rest_q > 0.0f) {
+        const float apart = o.gap / o.rest_q;                        // p_r / q_r - 1
+        sum += o.rest_q * above_log(apart);
+    } else {
+        sum += o.rest_p + (o.mass - 1.0f);
+    }
+    if (at_row.there && q0 == 0) loss[first + threadIdx.x / LANES] = at_row.live && o.soft.total != 0.0f && o.listed ? tau * tau * sum : 0.0f;
+    lds_order();
 }
 
 template <typename T, int LANES, int VPL, bool VEC, int NK>
@@ -192,38 +191,29 @@ __global__ __launch_bounds__(256) void route_distill_backward_kernel(const T *__
     const int q0 = threadIdx.x % LANES;
     float *mine = lds + threadIdx.x / LANES * (LANES * VPL);
     const float inv_tau = 1.0f / tau;
-    const int64_t stride = (int64_t)gridDim.x * ROWS_PER_BLOCK;
-    for (int64_t first = (int64_t)blockIdx.x * ROWS_PER_BLOCK; first < rows; first += stride) {
-        const RowAt at_row = row_at(threadIdx.x / LANES, rows - first, row_mask, first);
-        Distilled<LANES, VPL, NK> o;
-        distill_row<T, LANES, VPL, VEC, NK>(logits, first, at_row, E, ld, inv_tau, t_idx, t_logit, t_lse, K, q0, mine, o);
-        const bool counts = at_row.live && o.soft.total != 0.0f;
-        const float along = d_loss[first + at_row.slot];
-        lds_order();
-        lds_put<LANES, NK>(mine, q0, K, o.at, o.again, o.q);
-        float listed[VPL];
-        lds_values<LANES, VPL, VEC>(mine, q0, listed);
-        lds_order();
-        const float unit = tau * along;
-        const float scale = inverse(o.soft.total);
-        const float inside = (o.mass + o.rest_q) * scale;
-        // Q + q_r - q_r / p_r is (p_r - q_r) / p_r where sum q + q_r is 1
-        const float outside = (o.rest_q > 0.0f ? o.gap / o.rest_p : o.mass) * scale;
+    const int64_t first = first_row(ROWS_PER_BLOCK);
+    if (first >= rows) return;
+    const RowAt at_row = row_at(threadIdx.x / LANES, rows - first, row_mask, first);
+    Distilled<LANES, VPL, NK> o;
+    distill_row<T, LANES, VPL, VEC, NK>(logits, first, at_row, E, ld, inv_tau, t_idx, t_logit, t_lse, K, q0, mine, o);
+    const bool counts = at_row.live && o.soft.total != 0.0f;
+    const float along = d_loss[first + at_row.slot];
+    lds_order();
+    lds_put<LANES, NK>(mine, q0, K, o.at, o.again, o.q);
+    float listed[VPL];
+    lds_values<LANES, VPL, VEC>(mine, q0, listed);
+    lds_order();
+    const float unit = tau * along;
+    const float scale = inverse(o.soft.total);
+    const float inside = (o.mass + o.rest_q) * scale;
+    // Q + q_r - q_r / p_r is (p_r - q_r) / p_r where sum q + q_r is 1
+    const float outside = (o.rest_q > 0.0f ? o.gap / o.rest_p : o.mass) * scale;
 #pragma unroll
-        for (int j = 0; j < VPL; ++j) {
-            const float g = listed[j] < 0.0f ? o.e[j] * outside : o.e[j] * inside - listed[j];
-            o.y[j] = counts && o.listed ? unit * g : 0.0f;
-        }
-        if (at_row.there && (counts || !add)) row_store<T, LANES, VPL, VEC>(d_logits + (first + threadIdx.x / LANES) * ld_d, E, q0, add != 0, o.y);
+    for (int j = 0; j < VPL; ++j) {
+        const float g = listed[j] < 0.0f ? o.e[j] * outside : o.e[j] * inside - listed[j];
+        o.y[j] = counts && o.listed ? unit * g : 0.0f;
     }
-}
-
-template <typename F>
-static int launch_distill(int64_t rows, int lanes, F launch)
-{
-    const int64_t blocks = (rows + 256 / lanes - 1) / (256 / lanes);
-    launch(dim3((unsigned)(blocks < (1 << 22) ? blocks : 1 << 22)));
-    return launch_status();
+    if (at_row.there && (counts || !add)) row_store<T, LANES, VPL, VEC>(d_logits + (first + threadIdx.x / LANES) * ld_d, E, q0, add != 0, o.y);
 }
 
 static int check_distill(int64_t rows, int32_t E, const int32_t *t_idx, const float *t_logit, int32_t K)
@@ -251,10 +241,9 @@ extern "C" int railsched_route_distill(const void *logits, int32_t dtype, int64_
         return by_shape(E, in_fours<T>(logits, E, ld), [&](auto s) {
             using S = decltype(s);
             return by_entries<S>(K, [&](auto n) {
-                return launch_distill(rows, S::LANES, [&](dim3 grid) {
-                    hipLaunchKernelGGL((route_distill_kernel<T, S::LANES, S::VPL, S::VEC, decltype(n)::value>), grid, dim3(256), 0, st,
-                                       static_cast<const T *>(logits), rows, E, ld, temperature, row_mask, t_idx, t_logit, t_lse, K, loss);
-                });
+            hipLaunchKernelGGL((route_distill_kernel<T, S::LANES, S::VPL, S::VEC, decltype(n)::value>), row_grid(rows, 256 / S::LANES), dim3(256), 0, st,
+                                   static_cast<const T *>(logits), rows, E, ld, temperature, row_mask, t_idx, t_logit, t_lse, K, loss);
+                return launch_status();
             });
         });
     });
@@ -277,11 +266,10 @@ extern "C" int railsched_route_distill_backward(const void *logits, int32_t dtyp
         return by_shape(E, in_fours<T>(logits, E, ld) && in_fours<T>(d_logits, E, ld_d), [&](auto s) {
             using S = decltype(s);
             return by_entries<S>(K, [&](auto n) {
-                return launch_distill(rows, S::LANES, [&](dim3 grid) {
-                    hipLaunchKernelGGL((route_distill_backward_kernel<T, S::LANES, S::VPL, S::VEC, decltype(n)::value>), grid, dim3(256), 0, st,
-                                       static_cast<const T *>(logits), rows, E, ld, temperature, row_mask, t_idx, t_logit, t_lse, K, d_loss, accumulate,
-                                       static_cast<T *>(d_logits), ld_d);
-                });
+            hipLaunchKernelGGL((route_distill_backward_kernel<T, S::LANES, S::VPL, S::VEC, decltype(n)::value>), row_grid(rows, 256 / S::LANES), dim3(256), 0, st,
+                                   static_cast<const T *>(logits), rows, E, ld, temperature, row_mask, t_idx, t_logit, t_lse, K, d_loss, accumulate,
+                                   static_cast<T *>(d_logits), ld_d);
+                return launch_status();
             });
         });
     });

@@ -54,69 +54,68 @@ __global__ __launch_bounds__(256) void route_logprobs_kernel(const T *__restrict
     constexpr int ROWS_PER_BLOCK = 256 / LANES;
     const int q = threadIdx.x % LANES;
     const float c = inv_tau * kLog2e;
-    const int64_t stride = (int64_t)gridDim.x * ROWS_PER_BLOCK;
-    for (int64_t first = (int64_t)blockIdx.x * ROWS_PER_BLOCK; first < rows; first += stride) {          // the same for every lane
-        const RowAt at_row = row_at(threadIdx.x / LANES, rows - first, row_mask, first);
-        const bool there = at_row.there;
-        const int64_t row = first + threadIdx.x / LANES;
-        const T *__restrict__ from = row_of(logits + first * ld, at_row.slot, ld);
-        const int32_t *__restrict__ ask = topk_idx + first * k + at_row.slot * k;
-        int pick = -1;
-        if (k > 0) {                                     // a lane's first pick is fetched with the row
-            pick = ask[q < k ? q : 0];
-            if (pick >= E) pick = -1;
+    const int64_t first = first_row(ROWS_PER_BLOCK);
+    if (first >= rows) return;
+    const RowAt at_row = row_at(threadIdx.x / LANES, rows - first, row_mask, first);
+    const bool there = at_row.there;
+    const int64_t row = first + threadIdx.x / LANES;
+    const T *__restrict__ from = row_of(logits + first * ld, at_row.slot, ld);
+    const int32_t *__restrict__ ask = topk_idx + first * k + at_row.slot * k;
+    int pick = -1;
+    if (k > 0) {                                     // a lane's first pick is fetched with the row
+        pick = ask[q < k ? q : 0];
+        if (pick >= E) pick = -1;
+    }
+    float x[VPL], dot;
+    row_values<T, LANES, VPL, VEC>(from, E, q, x);
+    const float picked = (float)from[pick < 0 ? 0 : pick];
+    const RowSoft soft = row_sums<LANES, VPL>(x, c, dot);
+    const bool counts = at_row.live && soft.total != 0.0f;
+    const float log_total = log2_of(soft.total);
+    if (there && q == 0) {
+        if (lse) lse[row] = counts ? fmaf(soft.largest, inv_tau, kLn2 * log_total) : 0.0f;
+        if (entropy) entropy[row] = counts ? kLn2 * (log_total - dot * inverse(soft.total)) : 0.0f;
+    }
+    if (there && q < k) logp[row * k + q] = counts && pick >= 0 ? kLn2 * (soft.y(picked, c) - log_total) : 0.0f;
+    if (there) {
+        for (int j = q + LANES; j < k; j += LANES) {
+            const int at = ask[j];
+            const bool good = counts && at >= 0 && at < E;
+            logp[row * k + j] = good ? kLn2 * (soft.y((float)from[at], c) - log_total) : 0.0f;
         }
-        float x[VPL], dot;
-        row_values<T, LANES, VPL, VEC>(from, E, q, x);
-        const float picked = (float)from[pick < 0 ? 0 : pick];
-        const RowSoft soft = row_sums<LANES, VPL>(x, c, dot);
-        const bool counts = at_row.live && soft.total != 0.0f;
-        const float log_total = log2_of(soft.total);
-        if (there && q == 0) {
-            if (lse) lse[row] = counts ? fmaf(soft.largest, inv_tau, kLn2 * log_total) : 0.0f;
-            if (entropy) entropy[row] = counts ? kLn2 * (log_total - dot * inverse(soft.total)) : 0.0f;
-        }
-        if (there && q < k) logp[row * k + q] = counts && pick >= 0 ? kLn2 * (soft.y(picked, c) - log_total) : 0.0f;
-        if (there) {
-            for (int j = q + LANES; j < k; j += LANES) {
-                const int at = ask[j];
-                const bool good = counts && at >= 0 && at < E;
-                logp[row * k + j] = good ? kLn2 * (soft.y((float)from[at], c) - log_total) : 0.0f;
-            }
-        }
-        if constexpr (ALT != ALT_NONE) {
-            auto put = [&](int sel, int at) {            // an alternative: its logit once more, from the cache
-                const float v = at < E ? (float)from[at] : -INFINITY;
-                const bool good = counts && v != -INFINITY;
-                alt_idx[row * m + sel] = good ? at : -1;
-                alt_logp[row * m + sel] = good ? kLn2 * (soft.y(v, c) - log_total) : counts ? -INFINITY : 0.0f;
-            };
-            auto each = [&](int sel, int at) {
-                if (there && q == sel % LANES) put(sel, at);
-            };
-            if constexpr (ALT == ALT_ROUNDS) {
-                row_rounds<LANES, VPL, VEC>(x, m, q, each);
-            } else {
-                constexpr int KM = 8;
-                constexpr unsigned MASK = (unsigned)(LANES * VPL) - 1u;
-                float4 v[VPL / 4];
+    }
+    if constexpr (ALT != ALT_NONE) {
+        auto put = [&](int sel, int at) {            // an alternative: its logit once more, from the cache
+            const float v = at < E ? (float)from[at] : -INFINITY;
+            const bool good = counts && v != -INFINITY;
+            alt_idx[row * m + sel] = good ? at : -1;
+            alt_logp[row * m + sel] = good ? kLn2 * (soft.y(v, c) - log_total) : counts ? -INFINITY : 0.0f;
+        };
+        auto each = [&](int sel, int at) {
+            if (there && q == sel % LANES) put(sel, at);
+        };
+        if constexpr (ALT == ALT_ROUNDS) {
+            row_rounds<LANES, VPL, VEC>(x, m, q, each);
+        } else {
+            constexpr int KM = 8;
+            constexpr unsigned MASK = (unsigned)(LANES * VPL) - 1u;
+            float4 v[VPL / 4];
 #pragma unroll
-                for (int i = 0; i < VPL / 4; ++i) v[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-                int own[L];
-                unsigned bits, u[KM];
-                lane_best<LANES, VPL, L, false>(v, E, q, own, bits);
-                const bool bad = row_best<LANES, VPL, L, KM>(own, bits, m, u);
-                if (__ballot(there && bad) == 0ull) {
+            for (int i = 0; i < VPL / 4; ++i) v[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+            int own[L];
+            unsigned bits, u[KM];
+            lane_best<LANES, VPL, L, false>(v, E, q, own, bits);
+            const bool bad = row_best<LANES, VPL, L, KM>(own, bits, m, u);
+            if (__ballot(there && bad) == 0ull) {
 #pragma unroll
-                    for (int r = 0; r < (KM + LANES - 1) / LANES; ++r) {     // alternatives q, q + LANES, ... of this lane
-                        unsigned sel = 0;
+                for (int r = 0; r < (KM + LANES - 1) / LANES; ++r) {     // alternatives q, q + LANES, ... of this lane
+                    unsigned sel = 0;
 #pragma unroll
-                        for (int j = r * LANES; j < KM && j < (r + 1) * LANES; ++j) sel = j == q + r * LANES ? u[j] : sel;
-                        if (there && q + r * LANES < m) put(q + r * LANES, (int)key_index<MASK>(sel));
-                    }
-                } else {
-                    row_rounds<LANES, VPL, VEC>(x, m, q, each);
+                    for (int j = r * LANES; j < KM && j < (r + 1) * LANES; ++j) sel = j == q + r * LANES ? u[j] : sel;
+                    if (there && q + r * LANES < m) put(q + r * LANES, (int)key_index<MASK>(sel));
                 }
+            } else {
+                row_rounds<LANES, VPL, VEC>(x, m, q, each);
             }
         }
     }
@@ -136,75 +135,70 @@ __global__ __launch_bounds__(256) void route_logprobs_backward_kernel(const T *_
     __shared__ __align__(16) float lds[ROWS_PER_BLOCK * LANES * VPL];
     const int q = threadIdx.x % LANES;
     float *mine = lds + threadIdx.x / LANES * (LANES * VPL);
-    const int64_t stride = (int64_t)gridDim.x * ROWS_PER_BLOCK;
-    for (int64_t first = (int64_t)blockIdx.x * ROWS_PER_BLOCK; first < rows; first += stride) {
-        const RowAt at_row = row_at(threadIdx.x / LANES, rows - first, row_mask, first);
-        float y[VPL], e[VPL];
-        row_values<T, LANES, VPL, VEC>(row_of(logits + first * ld, at_row.slot, ld), E, q, y);
-        const int64_t entry0 = first * k + at_row.slot * k;
-        const float along = d_lse ? d_lse[first + at_row.slot] : 0.0f;
-        const float spread = d_entropy ? kLn2 * d_entropy[first + at_row.slot] : 0.0f;
+    const int64_t first = first_row(ROWS_PER_BLOCK);
+    if (first >= rows) return;
+    const RowAt at_row = row_at(threadIdx.x / LANES, rows - first, row_mask, first);
+    float y[VPL], e[VPL];
+    row_values<T, LANES, VPL, VEC>(row_of(logits + first * ld, at_row.slot, ld), E, q, y);
+    const int64_t entry0 = first * k + at_row.slot * k;
+    const float along = d_lse ? d_lse[first + at_row.slot] : 0.0f;
+    const float spread = d_entropy ? kLn2 * d_entropy[first + at_row.slot] : 0.0f;
 
-        float dx[VPL], sum = 0.0f;
+    float dx[VPL], sum = 0.0f;
 #pragma unroll
-        for (int j = 0; j < VPL; ++j) dx[j] = 0.0f;
-        if (d_logp) {
-            for (int j0 = 0; j0 < k; j0 += LANES * NK) {             // NK entries a lane at a time
-                int at[NK];
-                bool again[NK];
-                float g[NK], part[VPL];
+    for (int j = 0; j < VPL; ++j) dx[j] = 0.0f;
+    if (d_logp) {
+        for (int j0 = 0; j0 < k; j0 += LANES * NK) {             // NK entries a lane at a time
+            int at[NK];
+            bool again[NK];
+            float g[NK], part[VPL];
 #pragma unroll
-                for (int r = 0; r < NK; ++r) {
-                    const int j = j0 + q + LANES * r;
-                    const int64_t entry = entry0 + (j < k ? j : 0);
-                    at[r] = topk_idx[entry];
-                    g[r] = d_logp[entry];
-                    if (j >= k || at[r] >= E) at[r] = -1;
-                    if (at[r] < 0) g[r] = 0.0f;
-                    sum += g[r];
-                }
-                lds_fill<LANES, VPL, VEC>(mine, q, 0.0f);
-                lds_order();
-                lds_mark<LANES, NK>(mine, q, k - j0, at, again);
-                lds_put<LANES, NK>(mine, q, k - j0, at, again, g);
-                lds_values<LANES, VPL, VEC>(mine, q, part);
-                lds_order();
-#pragma unroll
-                for (int j = 0; j < VPL; ++j) dx[j] += part[j];
+            for (int r = 0; r < NK; ++r) {
+                const int j = j0 + q + LANES * r;
+                const int64_t entry = entry0 + (j < k ? j : 0);
+                at[r] = topk_idx[entry];
+                g[r] = d_logp[entry];
+                if (j >= k || at[r] >= E) at[r] = -1;
+                if (at[r] < 0) g[r] = 0.0f;
+                sum += g[r];
             }
-            sum = row_sum<LANES>(sum);
+            lds_fill<LANES, VPL, VEC>(mine, q, 0.0f);
+            lds_order();
+            lds_mark<LANES, NK>(mine, q, k - j0, at, again);
+            lds_put<LANES, NK>(mine, q, k - j0, at, again, g);
+            lds_values<LANES, VPL, VEC>(mine, q, part);
+            lds_order();
+#pragma unroll
+            for (int j = 0; j < VPL; ++j) dx[j] += part[j];
         }
-        const RowSoft soft = row_softmax<LANES, VPL>(y, e, inv_tau * kLog2e);
-        const bool counts = at_row.live && soft.total != 0.0f;
-        const float scale = inverse(soft.total), pull = sum - along;
-        if (d_entropy) {
-            const float mean = row_dot<LANES, VPL>(y, e) * scale;
-#pragma unroll
-            for (int j = 0; j < VPL; ++j) dx[j] -= e[j] * scale * (pull + spread * (fmaxf(y[j], -1e30f) - mean));
-        } else {
-#pragma unroll
-            for (int j = 0; j < VPL; ++j) dx[j] -= e[j] * scale * pull;
-        }
-#pragma unroll
-        for (int j = 0; j < VPL; ++j) dx[j] = counts ? dx[j] * inv_tau : 0.0f;
-        if (at_row.there && (counts || !add)) row_store<T, LANES, VPL, VEC>(d_logits + (first + threadIdx.x / LANES) * ld_d, E, q, add != 0, dx);
+        sum = row_sum<LANES>(sum);
     }
+    const RowSoft soft = row_softmax<LANES, VPL>(y, e, inv_tau * kLog2e);
+    const bool counts = at_row.live && soft.total != 0.0f;
+    const float scale = inverse(soft.total), pull = sum - along;
+    if (d_entropy) {
+        const float mean = row_dot<LANES, VPL>(y, e) * scale;
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) dx[j] -= e[j] * scale * (pull + spread * (fmaxf(y[j], -1e30f) - mean));
+    } else {
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) dx[j] -= e[j] * scale * pull;
+    }
+#pragma unroll
+    for (int j = 0; j < VPL; ++j) dx[j] = counts ? dx[j] * inv_tau : 0.0f;
+    if (at_row.there && (counts || !add)) row_store<T, LANES, VPL, VEC>(d_logits + (first + threadIdx.x / LANES) * ld_d, E, q, add != 0, dx);
 }
 
 template <typename T, int LANES, int VPL, bool VEC, int ALT, int L, typename... A>
 static int launch_logprobs(const T *logits, int64_t rows, hipStream_t st, A... rest)
 {
-    const int64_t blocks = (rows + 256 / LANES - 1) / (256 / LANES);
-    hipLaunchKernelGGL((route_logprobs_kernel<T, LANES, VPL, VEC, ALT, L>), dim3((unsigned)(blocks < (1 << 22) ? blocks : 1 << 22)), dim3(256), 0, st, logits, rows,
-                       rest...);
+    hipLaunchKernelGGL((route_logprobs_kernel<T, LANES, VPL, VEC, ALT, L>), row_grid(rows, 256 / LANES), dim3(256), 0, st, logits, rows, rest...);
     return launch_status();
 }
 template <typename T, int LANES, int VPL, bool VEC, int NK, typename... A>
 static int launch_logprobs_backward(const T *logits, int64_t rows, hipStream_t st, A... rest)
 {
-    const int64_t blocks = (rows + 256 / LANES - 1) / (256 / LANES);
-    hipLaunchKernelGGL((route_logprobs_backward_kernel<T, LANES, VPL, VEC, NK>), dim3((unsigned)(blocks < (1 << 22) ? blocks : 1 << 22)), dim3(256), 0, st,
-                       logits, rows, rest...);
+    hipLaunchKernelGGL((route_logprobs_backward_kernel<T, LANES, VPL, VEC, NK>), row_grid(rows, 256 / LANES), dim3(256), 0, st, logits, rows, rest...);
     return launch_status();
 }
 

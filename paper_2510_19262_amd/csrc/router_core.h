@@ -76,6 +76,15 @@ __device__ __forceinline__ bool row_any(bool v)
     else return ((all >> (threadIdx.x & 63u & ~(unsigned)(LANES - 1))) & ((1ull << LANES) - 1ull)) != 0ull;
 }
 
+// ---- the first of a workgroup's `each` rows.  A grid covers all rows, in two dimensions where one would have more work-items than 32 bits count; a loop over
+// the rows instead would keep every loop-invariant condition in scalar registers, and spill them.
+__device__ __forceinline__ int64_t first_row(int each) { return ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * each; }
+inline dim3 row_grid(int64_t rows, int each)
+{
+    const int64_t blocks = (rows + each - 1) / each, wide = 1 << 22;
+    return blocks <= wide ? dim3((unsigned)blocks) : dim3((unsigned)wide, (unsigned)((blocks + wide - 1) / wide));
+}
+
 // ---- which row the lanes are at.  A workgroup has the rows first, first + 1, ... in hand, one to LANES lanes, of which `left` exist.  Lanes without a row, and
 // lanes whose row is masked, follow the workgroup's first row instead: their loads need no branch (a load under a condition is waited for before
 // the next one is made), read what is read anyway, and what comes of them is not used.
