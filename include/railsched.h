@@ -312,7 +312,7 @@ int railsched_port_round_robin(const int64_t *chunk_off, const uint8_t *rail, in
  *             between the rows are left as they are.  accumulate = 0: overwritten; 1: added to what is there (each
  *             sum rounded to `dtype`; rows that do not count are left as they are).
  *   An index outside [0,E) is ignored.
- * Limits: E <= 1024, k, m and K <= E, m and K <= 64, rows < 2^31, ld and ld_d <= 2^31.  rows may be 0 (nothing is written but the groups' outputs).
+ * Limits: E <= 1024, k, m and K <= E, m and K <= 64, rows < 2^31, ld and ld_d <= 2^31, groups <= 2^23.  rows may be 0 (nothing is written but the groups' outputs).
  * Errors: NULL_PTR, INVALID_ARG (sizes, ld < E, unknown dtype, temperature out of range, accumulate not 0 or 1,
  * d_logits == logits), UNSUPPORTED (limits), WORKSPACE.
  * ------------------------------------------------------------------------------------------- */

@@ -35,6 +35,7 @@ struct Records {
     __device__ __forceinline__ float *at(int64_t slice, int64_t group) const { return data + (slice + group) * words; }
 };
 
+constexpr int kMaxGroups = 1 << 23;                     // a workgroup each, within the work-items that a grid counts
 constexpr int kTile = 32;                               // columns that a workgroup of the joining kernel adds up
 
 // v added up over the lanes that are a multiple of LANES away from this one, in all of them
@@ -104,7 +105,7 @@ __global__ __launch_bounds__(256) void route_balance_kernel(const T *__restrict_
             const int32_t *__restrict__ chosen = topk_idx + w0 * k + at_row.slot * k;
             const int pick = chosen[q < k ? q : 0];                  // a lane's first pick is fetched with the row
             float t[VPL], e[VPL];
-            row_values<T, LANES, VPL, VEC>(row_of(logits + w0 * ld, at_row.slot, ld), E, q, t);
+            row_values<false, T, LANES, VPL, VEC>(row_of(logits + w0 * ld, at_row.slot, ld), E, q, t);
             const RowSoft soft = row_softmax<LANES, VPL>(t, e, kLog2e);
             const bool use = at_row.live && soft.total != 0.0f;
             const float scale = inverse(soft.total);
@@ -216,7 +217,7 @@ __global__ __launch_bounds__(THREADS) void route_balance_join_kernel(Records rec
 template <typename T, int LANES, int VPL, bool VEC>
 __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__restrict__ logits, int E, int64_t ld,
                                                                      const uint8_t *__restrict__ row_mask, int k, Groups groups,
-                                                                     int64_t slice_rows, float coef, const int64_t *__restrict__ counts,
+                                                                     int slice_rows, float coef, const int64_t *__restrict__ counts,
                                                                      const int64_t *__restrict__ tokens, const float *__restrict__ d_loss,
                                                                      int add, T *__restrict__ d_logits, int64_t ld_d)
 {
@@ -224,7 +225,8 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
     __shared__ double part[4], total;
     __shared__ float weight[LANES * VPL];
     const int q = threadIdx.x % LANES, slot = threadIdx.x / LANES;
-    const int64_t r0 = blockIdx.x * slice_rows;
+    const int64_t r0 = first_row(slice_rows);
+    if (r0 >= groups.rows) return;
     const int64_t r1 = r0 + slice_rows < groups.rows ? r0 + slice_rows : groups.rows;
     for (int g = groups.first(r0); g < groups.n; ++g) {
         const int64_t gb = groups.begin(g), ge = groups.begin(g + 1);
@@ -232,6 +234,10 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
         const int64_t lo = gb > r0 ? gb : r0, hi = ge < r1 ? ge : r1;
         if (lo >= hi) continue;
         const int64_t *__restrict__ c = counts + (int64_t)g * E;
+        // the first rows in hand are on their way while the weights are formed
+        RowAt at_row = row_at(slot, hi - lo, row_mask, lo);
+        float t[VPL];
+        row_values<false, T, LANES, VPL, VEC>(row_of(logits + lo * ld, at_row.slot, ld), E, q, t);
         double sum = 0.0;
         for (int i = threadIdx.x; i < E; i += 256) sum += (double)c[i];
         sum = block_sum<4>(sum, part);
@@ -248,9 +254,7 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
             a[j] = i < E ? weight[i] : 0.0f;
         }
         for (int64_t w0 = lo; w0 < hi; w0 += ROWS_PER_BLOCK) {
-            const RowAt at_row = row_at(slot, hi - w0, row_mask, w0);
-            float t[VPL], e[VPL];
-            row_values<T, LANES, VPL, VEC>(row_of(logits + w0 * ld, at_row.slot, ld), E, q, t);
+            float e[VPL];
             const RowSoft soft = row_softmax<LANES, VPL>(t, e, kLog2e);
             const bool counts_here = at_row.live && soft.total != 0.0f;
             const float scale = inverse(soft.total);
@@ -264,6 +268,10 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
 #pragma unroll
             for (int j = 0; j < VPL; ++j) t[j] = counts_here ? e[j] * (a[j] - ap) : 0.0f;
             if (at_row.there && (counts_here || !add)) row_store<T, LANES, VPL, VEC>(d_logits + (w0 + slot) * ld_d, E, q, add != 0, t);
+            if (w0 + ROWS_PER_BLOCK < hi) {
+                at_row = row_at(slot, hi - (w0 + ROWS_PER_BLOCK), row_mask, w0 + ROWS_PER_BLOCK);
+                row_values<false, T, LANES, VPL, VEC>(row_of(logits + (w0 + ROWS_PER_BLOCK) * ld, at_row.slot, ld), E, q, t);
+            }
         }
         __syncthreads();
     }
@@ -277,6 +285,16 @@ static int64_t balance_slice_rows(int64_t rows, int E)
     return r > least ? r : least;
 }
 static int64_t balance_slices(int64_t rows, int E) { return (rows + balance_slice_rows(rows, E) - 1) / balance_slice_rows(rows, E); }
+// Rows of a workgroup of the gradient: 16 KiB of logits, 32 KiB of rows of more than 256 bytes; whole rounds of the rows in hand; fewer where the GPU would not be full.  Much
+// more is slower by up to a third (2^20 x 256: 344 us with 32 KiB, 417 with 512; 2^21 x 64: 179 with 16, 235 with 256), less pays for the weights too often (2^23 x 8: 839 us
+// with 0.5 KiB, 92 with 16).
+static int gradient_slice_rows(int64_t rows, int row_bytes, int in_hand)
+{
+    int64_t r = (row_bytes <= 256 ? 16384 : 32768) / row_bytes;
+    if (r > rows / 2048) r = rows / 2048;
+    r -= r % in_hand;
+    return r > in_hand ? (int)r : in_hand;
+}
 static int balance_tiles(int E) { return (E + kTile - 1) / kTile; }
 
 static size_t records_bytes(int64_t rows, int32_t groups, int32_t E)
@@ -287,6 +305,7 @@ static size_t tickets_bytes(int32_t groups) { return align_up((size_t)groups * s
 
 static int check_groups(int64_t rows, const int64_t *group_off, int32_t groups)
 {
+    if (groups > kMaxGroups) return RAILSCHED_ERR_UNSUPPORTED;
     if (groups < 0 || (!group_off && (groups == 0 ? rows != 0 : rows % groups != 0))) return RAILSCHED_ERR_INVALID_ARG;
     return RAILSCHED_OK;
 }
@@ -305,7 +324,7 @@ static Groups make_groups(int64_t rows, const int64_t *group_off, int32_t groups
 extern "C" size_t railsched_route_balance_workspace_bytes(int64_t rows, int32_t groups, int32_t E)
 {
     using namespace rs;
-    if (rows < 0 || rows > 0x7FFFFFFFll || groups < 0 || E < 1 || E > kMaxExperts) return 0;
+    if (rows < 0 || rows > 0x7FFFFFFFll || groups < 0 || groups > kMaxGroups || E < 1 || E > kMaxExperts) return 0;
     return records_bytes(rows, groups, E) + tickets_bytes(groups) + align_up((size_t)groups * balance_tiles(E) * sizeof(double), 256);
 }
 
@@ -377,8 +396,9 @@ extern "C" int railsched_route_balance_backward(const void *logits, int32_t dtyp
         using T = decltype(t);
         return by_shape(E, in_fours<T>(logits, E, ld) && in_fours<T>(d_logits, E, ld_d), [&](auto s) {
             using S = decltype(s);
-            hipLaunchKernelGGL((route_balance_backward_kernel<T, S::LANES, S::VPL, S::VEC>), dim3((unsigned)balance_slices(rows, E)), dim3(256), 0, st,
-                               static_cast<const T *>(logits), E, ld, row_mask, k, gr, balance_slice_rows(rows, E), coef, counts, tokens, d_loss,
+            const int slice_rows = gradient_slice_rows(rows, (int)sizeof(T) * E, 256 / S::LANES);
+            hipLaunchKernelGGL((route_balance_backward_kernel<T, S::LANES, S::VPL, S::VEC>), row_grid(rows, slice_rows), dim3(256), 0, st,
+                               static_cast<const T *>(logits), E, ld, row_mask, k, gr, slice_rows, coef, counts, tokens, d_loss,
                                accumulate, static_cast<T *>(d_logits), ld_d);
             return launch_status();
         });

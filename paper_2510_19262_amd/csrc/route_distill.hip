@@ -77,7 +77,7 @@ __device__ __forceinline__ void distill_row(const T *__restrict__ logits, int64_
         }
     }
     const float teacher = t_lse ? t_lse[first + at_row.slot] : 0.0f;
-    row_values<T, LANES, VPL, VEC>(from, E, q0, o.y);
+    row_values<true, T, LANES, VPL, VEC>(from, E, q0, o.y);
     float best = -INFINITY;
     bool any = false;
 #pragma unroll

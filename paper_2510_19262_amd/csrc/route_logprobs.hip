@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256) void route_logprobs_kernel(const T *__restrict
         if (pick >= E) pick = -1;
     }
     float x[VPL], dot;
-    row_values<T, LANES, VPL, VEC>(from, E, q, x);
+    row_values<true, T, LANES, VPL, VEC>(from, E, q, x);
     const float picked = (float)from[pick < 0 ? 0 : pick];
     const RowSoft soft = row_sums<LANES, VPL>(x, c, dot);
     const bool counts = at_row.live && soft.total != 0.0f;
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(256) void route_logprobs_backward_kernel(const T *_
     if (first >= rows) return;
     const RowAt at_row = row_at(threadIdx.x / LANES, rows - first, row_mask, first);
     float y[VPL], e[VPL];
-    row_values<T, LANES, VPL, VEC>(row_of(logits + first * ld, at_row.slot, ld), E, q, y);
+    row_values<false, T, LANES, VPL, VEC>(row_of(logits + first * ld, at_row.slot, ld), E, q, y);
     const int64_t entry0 = first * k + at_row.slot * k;
     const float along = d_lse ? d_lse[first + at_row.slot] : 0.0f;
     const float spread = d_entropy ? kLn2 * d_entropy[first + at_row.slot] : 0.0f;

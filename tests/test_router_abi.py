@@ -91,6 +91,7 @@ def test_balance_validation():
     assert call(k=0) == -1 and call(k=9) == -1 and call(groups=-1) == -1
     assert call(groups=3) == -1                                              # 1000 rows in three equal parts
     assert call(groups=0) == -1                                              # rows, but no group
+    assert call(off=D, groups=(1 << 23) + 1) == -3 and lib.railsched_route_balance_workspace_bytes(1000, (1 << 23) + 1, 8) == 0
     for n in ("counts", "tokens", "prob_sum", "loss"):
         assert call(**{n: None}) == -2
     assert call(ws=None) == -5 and call(ws_bytes=need - 1) == -5 and call(ws=P(0x1010)) == -5
