@@ -13,17 +13,49 @@ struct Groups {
     const int64_t *off;     // NULL: equal parts of `each` rows
     int64_t each, rows;
     int n;
-    __device__ __forceinline__ int64_t begin(int g) const
-    {
-        const int64_t b = off ? off[g] : g * each;
-        return b < 0 ? 0 : b < rows ? b : rows;
-    }
-    // the first group that can hold a row >= r; by all lanes of a wavefront
-    __device__ __forceinline__ int first(int64_t r) const
+    __device__ __forceinline__ int64_t within(int64_t b) const { return b < 0 ? 0 : b < rows ? b : rows; }
+    __device__ __forceinline__ int64_t begin(int g) const { return within(off ? off[g] : g * each); }
+    // the last group that begins at r or before, the first one if none does: 64 probes a step by the lanes of a wavefront
+    __device__ __forceinline__ int holding(int64_t r) const
     {
         if (!off) return (int)(r / each);
-        return off[0] > r ? 0 : wave_last_le(off, n, r);
+        const int lane = threadIdx.x & 63;
+        int lo = 0, hi = n;
+        while (hi - lo > 1) {
+            const int step = (hi - lo + 63) / 64;
+            const int at = lo + lane * step;
+            const unsigned long long ok = __ballot(at < hi && off[at < hi ? at : lo] <= r);
+            if (ok == 0ull) return lo;
+            lo += (63 - __clzll((long long)ok)) * step;
+            hi = lo + step < hi ? lo + step : hi;
+        }
+        return lo;
     }
+};
+
+// The groups from `first` on, one after the other: their offsets are fetched 63 groups at a time, a lane each.
+struct GroupWalk {
+    int g, base;
+    int64_t held;           // this lane's offset: of group base + lane
+    __device__ __forceinline__ void fetch(const Groups &groups)
+    {
+        base = g;
+        const int at = g + (int)(threadIdx.x & 63);
+        held = groups.begin(at <= groups.n ? at : groups.n);
+    }
+    __device__ __forceinline__ GroupWalk(const Groups &groups, int first) : g(first) { fetch(groups); }
+    __device__ __forceinline__ void next(const Groups &groups)
+    {
+        if (++g - base == 63 && g < groups.n) fetch(groups);
+    }
+    __device__ __forceinline__ int64_t lane(int i) const
+    {
+        const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(uint32_t)(uint64_t)held, i);
+        const unsigned hi = (unsigned)__builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)held >> 32), i);
+        return (int64_t)(((uint64_t)hi << 32) | lo);
+    }
+    __device__ __forceinline__ int64_t begin() const { return lane(g - base); }
+    __device__ __forceinline__ int64_t end() const { return lane(g - base + 1); }
 };
 
 // The workspace: a record for every part (E sums, E counts, the rows that count), the tickets of the groups, and the products of their column tiles.
@@ -71,41 +103,52 @@ __device__ __forceinline__ float balance_loss(float coef, int E, int k, int64_t 
 }
 
 // DIRECT: every slice is a whole group, whose outputs leave from here.
-template <typename T, int LANES, int VPL, bool VEC, bool DIRECT>
-__global__ __launch_bounds__(256) void route_balance_kernel(const T *__restrict__ logits, int E, int64_t ld, const uint8_t *__restrict__ row_mask,
+template <typename T, int LANES, int VPL, bool VEC, int THREADS, bool DIRECT>
+__global__ __launch_bounds__(THREADS) void route_balance_kernel(const T *__restrict__ logits, int E, int64_t ld, const uint8_t *__restrict__ row_mask,
                                                             const int32_t *__restrict__ topk_idx, int k, Groups groups, int64_t slice_rows, float coef,
                                                             Records records, int64_t *__restrict__ counts, int64_t *__restrict__ tokens,
                                                             float *__restrict__ prob_sum, float *__restrict__ loss)
 {
-    constexpr int ROWS_PER_BLOCK = 256 / LANES;
-    __shared__ float sums[4][LANES * VPL];
+    constexpr int ROWS_PER_BLOCK = THREADS / LANES, WAVES = THREADS / 64;
+    __shared__ float sums[WAVES][LANES * VPL];
     __shared__ unsigned picks[LANES * VPL];
     __shared__ unsigned counted;
-    __shared__ double part[4];
+    __shared__ double part[WAVES];
     const int q = threadIdx.x % LANES, slot = threadIdx.x / LANES, wave = threadIdx.x >> 6;
     const int64_t r0 = blockIdx.x * slice_rows;
     const int64_t r1 = r0 + slice_rows < groups.rows ? r0 + slice_rows : groups.rows;
     if constexpr (!DIRECT) {
-        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < groups.n; i += (int64_t)gridDim.x * 256) records.tickets[i] = 0;
+        for (int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x; i < groups.n; i += (int64_t)gridDim.x * THREADS) records.tickets[i] = 0;
     }
-    for (int g = groups.first(r0); g < groups.n; ++g) {
-        const int64_t gb = groups.begin(g), ge = groups.begin(g + 1);
+    for (GroupWalk walk(groups, groups.holding(r0)); walk.g < groups.n; walk.next(groups)) {
+        const int g = walk.g;
+        const int64_t gb = walk.begin(), ge = walk.end();
         if (gb >= r1) break;
         const int64_t lo = gb > r0 ? gb : r0, hi = ge < r1 ? ge : r1;
         if (lo >= hi) continue;
-        for (int i = threadIdx.x; i < E; i += 256) picks[i] = 0;
+        for (int i = threadIdx.x; i < E; i += THREADS) picks[i] = 0;
         if (threadIdx.x == 0) counted = 0;
         __syncthreads();
         float acc[VPL];
 #pragma unroll
         for (int j = 0; j < VPL; ++j) acc[j] = 0.0f;
         unsigned here = 0;
+        // the rows in hand, with a lane's first pick; the next ones are on their way while these are worked on (2^25 x 8: 218 us, 241 without; 2^20 x 256 bf16 123, 157)
+        RowAt at_next;
+        RowRaw<T, VPL, VEC> raw;
+        int pick_next;
+        auto fetch = [&](int64_t w) {
+            at_next = row_at(slot, hi - w, row_mask, w);
+            pick_next = topk_idx[w * k + at_next.slot * k + (q < k ? q : 0)];
+            row_fetch<false, T, LANES, VPL, VEC>(row_of(logits + w * ld, at_next.slot, ld), E, q, raw);
+        };
+        fetch(lo);
         for (int64_t w0 = lo; w0 < hi; w0 += ROWS_PER_BLOCK) {
-            const RowAt at_row = row_at(slot, hi - w0, row_mask, w0);
-            const int32_t *__restrict__ chosen = topk_idx + w0 * k + at_row.slot * k;
-            const int pick = chosen[q < k ? q : 0];                  // a lane's first pick is fetched with the row
+            const RowAt at_row = at_next;
+            const int pick = pick_next;
             float t[VPL], e[VPL];
-            row_values<false, T, LANES, VPL, VEC>(row_of(logits + w0 * ld, at_row.slot, ld), E, q, t);
+            row_take<T, LANES, VPL, VEC>(raw, E, q, t);
+            if (w0 + ROWS_PER_BLOCK < hi) fetch(w0 + ROWS_PER_BLOCK);
             const RowSoft soft = row_softmax<LANES, VPL>(t, e, kLog2e);
             const bool use = at_row.live && soft.total != 0.0f;
             const float scale = inverse(soft.total);
@@ -115,7 +158,7 @@ __global__ __launch_bounds__(256) void route_balance_kernel(const T *__restrict_
                 here += q == 0;
                 if (q < k && pick >= 0 && pick < E) atomicAdd(&picks[pick], 1u);
                 for (int j = q + LANES; j < k; j += LANES) {
-                    const int at = chosen[j];
+                    const int at = topk_idx[w0 * k + at_row.slot * k + j];
                     if (at >= 0 && at < E) atomicAdd(&picks[at], 1u);
                 }
             }
@@ -127,23 +170,29 @@ __global__ __launch_bounds__(256) void route_balance_kernel(const T *__restrict_
             if ((threadIdx.x & 63) < LANES) sums[wave][slot_index<LANES, VPL, VEC>(q, j)] = s;
         }
         __syncthreads();
+        auto wave_sums = [&](int i) {
+            float s = sums[0][i];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) s += sums[w][i];
+            return s;
+        };
         if constexpr (DIRECT) {
             double dot = 0.0;
-            for (int i = threadIdx.x; i < E; i += 256) {
-                const float s = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
+            for (int i = threadIdx.x; i < E; i += THREADS) {
+                const float s = wave_sums(i);
                 prob_sum[(int64_t)g * E + i] = s;
                 counts[(int64_t)g * E + i] = picks[i];
                 dot += (double)s * picks[i];
             }
-            dot = block_sum<4>(dot, part);
+            dot = block_sum<WAVES>(dot, part);
             if (threadIdx.x == 0) {
                 tokens[g] = counted;
                 loss[g] = balance_loss(coef, E, k, counted, dot);
             }
         } else {
             float *rec = records.at(blockIdx.x, g);
-            for (int i = threadIdx.x; i < E; i += 256) {
-                rec[i] = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
+            for (int i = threadIdx.x; i < E; i += THREADS) {
+                rec[i] = wave_sums(i);
                 reinterpret_cast<unsigned *>(rec)[E + i] = picks[i];
             }
             if (threadIdx.x == 0) reinterpret_cast<unsigned *>(rec)[2 * E] = counted;
@@ -228,8 +277,9 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
     const int64_t r0 = first_row(slice_rows);
     if (r0 >= groups.rows) return;
     const int64_t r1 = r0 + slice_rows < groups.rows ? r0 + slice_rows : groups.rows;
-    for (int g = groups.first(r0); g < groups.n; ++g) {
-        const int64_t gb = groups.begin(g), ge = groups.begin(g + 1);
+    for (GroupWalk walk(groups, groups.holding(r0)); walk.g < groups.n; walk.next(groups)) {
+        const int g = walk.g;
+        const int64_t gb = walk.begin(), ge = walk.end();
         if (gb >= r1) break;
         const int64_t lo = gb > r0 ? gb : r0, hi = ge < r1 ? ge : r1;
         if (lo >= hi) continue;
@@ -277,14 +327,24 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
     }
 }
 
-// rows of a slice: 2048 slices fill the GPU eight workgroups to a CU; no fewer than the rows that a workgroup has in hand at once, nor than 64, so that
-// the records stay few against the logits
-static int64_t balance_slice_rows(int64_t rows, int E)
+// How the rows are cut: whole rounds of the rows that a workgroup has in hand.  Workgroups of 256 threads, 2048 or some more of them, where the groups are short;
+// of 1024 threads, 512 or some more, where a group would have more than 16 records of the smaller ones, so that its records stay few.
+struct Cut {
+    int64_t slice_rows, slices;
+    int threads;
+};
+static Cut balance_cut(int64_t rows, int32_t groups, int E)
 {
-    const int64_t r = (rows + 2047) / 2048, least = E <= 8 ? 128 : 64;
-    return r > least ? r : least;
+    Cut c;
+    int64_t few = 1;
+    by_shape(E, true, [&](auto s) { return (int)(few = 256 / decltype(s)::LANES); });
+    for (c.threads = 256;; c.threads = 1024) {
+        const int64_t in_hand = few * (c.threads / 256), rounds = rows / (2048 * 256 / c.threads * in_hand);
+        c.slice_rows = (rounds > 1 ? rounds : 1) * in_hand;
+        c.slices = (rows + c.slice_rows - 1) / c.slice_rows;
+        if (c.threads == 1024 || c.slices <= 16 * (int64_t)groups) return c;
+    }
 }
-static int64_t balance_slices(int64_t rows, int E) { return (rows + balance_slice_rows(rows, E) - 1) / balance_slice_rows(rows, E); }
 // Rows of a workgroup of the gradient: 16 KiB of logits, 32 KiB of rows of more than 256 bytes; whole rounds of the rows in hand; fewer where the GPU would not be full.  Much
 // more is slower by up to a third (2^20 x 256: 344 us with 32 KiB, 417 with 512; 2^21 x 64: 179 with 16, 235 with 256), less pays for the weights too often (2^23 x 8: 839 us
 // with 0.5 KiB, 92 with 16).
@@ -299,7 +359,7 @@ static int balance_tiles(int E) { return (E + kTile - 1) / kTile; }
 
 static size_t records_bytes(int64_t rows, int32_t groups, int32_t E)
 {
-    return align_up((size_t)(balance_slices(rows, E) + groups + 1) * (2 * (size_t)E + 1) * sizeof(float), 256);
+    return align_up((size_t)(balance_cut(rows, groups, E).slices + groups + 1) * (2 * (size_t)E + 1) * sizeof(float), 256);
 }
 static size_t tickets_bytes(int32_t groups) { return align_up((size_t)groups * sizeof(unsigned), 256); }
 
@@ -344,7 +404,8 @@ extern "C" int railsched_route_balance(const void *logits, int32_t dtype, int64_
     const Groups gr = make_groups(rows, group_off, groups);
     // equal groups of few rows: a workgroup each, one launch and no records
     const bool direct = !group_off && rows > 0 && gr.each * E <= 16384;
-    const int64_t slice_rows = direct ? gr.each : balance_slice_rows(rows, E);
+    const Cut cut = balance_cut(rows, groups, E);
+    const int64_t slice_rows = direct ? gr.each : cut.slice_rows;
     Records records;
     records.data = static_cast<float *>(ws);
     records.words = 2 * (int64_t)E + 1;
@@ -356,19 +417,21 @@ extern "C" int railsched_route_balance(const void *logits, int32_t dtype, int64_
             using T = decltype(t);
             return by_shape(E, in_fours<T>(logits, E, ld), [&](auto s) {
                 using S = decltype(s);
-                if (direct)
-                    hipLaunchKernelGGL((route_balance_kernel<T, S::LANES, S::VPL, S::VEC, true>), grid, dim3(256), 0, st, static_cast<const T *>(logits), E,
-                                       ld, row_mask, topk_idx, k, gr, slice_rows, coef, records, counts, tokens, prob_sum, loss);
-                else
-                    hipLaunchKernelGGL((route_balance_kernel<T, S::LANES, S::VPL, S::VEC, false>), grid, dim3(256), 0, st, static_cast<const T *>(logits), E,
-                                       ld, row_mask, topk_idx, k, gr, slice_rows, coef, records, counts, tokens, prob_sum, loss);
+                auto go = [&](auto threads, auto whole) {
+                    hipLaunchKernelGGL((route_balance_kernel<T, S::LANES, S::VPL, S::VEC, decltype(threads)::value, decltype(whole)::value>), grid,
+                                       dim3(decltype(threads)::value), 0, st, static_cast<const T *>(logits), E, ld, row_mask, topk_idx, k, gr, slice_rows,
+                                       coef, records, counts, tokens, prob_sum, loss);
+                };
+                if (direct) go(std::integral_constant<int, 256>(), std::true_type());
+                else if (cut.threads == 256) go(std::integral_constant<int, 256>(), std::false_type());
+                else go(std::integral_constant<int, 1024>(), std::false_type());
                 return launch_status();
             });
         });
         if (rc || direct) return rc;
     }
     // a workgroup for every tile of columns where a group has many records; otherwise one for the group
-    const int64_t each = balance_slices(rows, E) / groups;
+    const int64_t each = cut.slices / groups;
     if (each > 16)
         hipLaunchKernelGGL(route_balance_join_kernel<1024>, dim3((unsigned)groups, (unsigned)balance_tiles(E)), dim3(1024), 0, st, records, E, k, gr, slice_rows,
                            coef, counts, tokens, prob_sum, loss);

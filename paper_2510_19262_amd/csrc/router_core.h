@@ -16,18 +16,15 @@ typedef _Float16 f16_t;
 
 constexpr int kMaxListed = 64;     // alternatives of a row, entries of a teacher's list
 
-// ---- four consecutive values: 16 bytes of fp32, 8 of the short types.  Streaming, but for rows some of whose logits are fetched again (AGAIN): those are to
-// stay in the L2 until then.  Gradient of the distillation of 2^20 x 256: 417 us streaming, 368 so; of the balance loss, which fetches nothing again: 423, 432.
-template <bool AGAIN, typename T>
+// ---- four consecutive values: 16 bytes of fp32, 8 of the short types
+template <typename T>
 __device__ __forceinline__ void load4(const T *p, float (&v)[4])
 {
     if constexpr (sizeof(T) == 4) {
-        const f32x4 *from = reinterpret_cast<const f32x4 *>(p);
-        const f32x4 x = AGAIN ? *from : __builtin_nontemporal_load(from);
+        const f32x4 x = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p));
         v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
     } else {
-        const u32x2 *from = reinterpret_cast<const u32x2 *>(p);
-        const u16x4 x = __builtin_bit_cast(u16x4, AGAIN ? *from : __builtin_nontemporal_load(from));
+        const u16x4 x = __builtin_bit_cast(u16x4, __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(p)));
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = (float)__builtin_bit_cast(T, (uint16_t)x[i]);
     }
@@ -112,28 +109,63 @@ __device__ __forceinline__ RowAt row_at(int slot, int64_t left, const uint8_t *_
 template <typename T>
 __device__ __forceinline__ T *row_of(T *first, int slot, int64_t ld) { return first + (uint64_t)(uint32_t)slot * (uint32_t)ld; }
 
-// This lane's values of a row as fp32; places behind the row are -infinity.
-// VEC: places of four consecutive experts, interleaved over the lanes, as slot_index() numbers them.
+// This lane's places of a row as they are in memory: fetched, and made fp32 values when they are needed (anything done to a loaded value waits for it).
+template <typename T, int VPL, bool VEC>
+struct RowRaw {
+    typedef typename std::conditional<sizeof(T) == 4, f32x4, u32x2>::type four;
+    typename std::conditional<VEC, four, T>::type v[VEC ? VPL / 4 : VPL];
+};
+// VEC: places of four consecutive experts, interleaved over the lanes, as slot_index() numbers them.  Streaming, but for rows some of whose logits are
+// fetched again (AGAIN): those are to stay in the L2 until then.  Gradient of the distillation of 2^20 x 256: 417 us streaming, 368 so; of the balance
+// loss, which fetches nothing again: 423, 432.
 template <bool AGAIN, typename T, int LANES, int VPL, bool VEC>
-__device__ __forceinline__ void row_values(const T *__restrict__ row, int E, int q, float (&x)[VPL])
+__device__ __forceinline__ void row_fetch(const T *__restrict__ row, int E, int q, RowRaw<T, VPL, VEC> &raw)
 {
     if constexpr (VEC) {
 #pragma unroll
         for (int c = 0; c < VPL / 4; ++c) {
-            float v[4];
             const int e0 = 4 * (q + LANES * c);
-            load4<AGAIN>(row + (e0 < E ? e0 : 0), v);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[4 * c + i] = e0 < E ? v[i] : -INFINITY;
+            const auto *from = reinterpret_cast<const typename RowRaw<T, VPL, VEC>::four *>(row + (e0 < E ? e0 : 0));
+            raw.v[c] = AGAIN ? *from : __builtin_nontemporal_load(from);
         }
     } else {
 #pragma unroll
         for (int j = 0; j < VPL; ++j) {
             const int e = q + LANES * j;
-            const float v = (float)row[e < E ? e : 0];
-            x[j] = e < E ? v : -INFINITY;
+            raw.v[j] = row[e < E ? e : 0];
         }
     }
+}
+// the values; places behind the row are -infinity
+template <typename T, int LANES, int VPL, bool VEC>
+__device__ __forceinline__ void row_take(const RowRaw<T, VPL, VEC> &raw, int E, int q, float (&x)[VPL])
+{
+    if constexpr (VEC) {
+#pragma unroll
+        for (int c = 0; c < VPL / 4; ++c) {
+            float v[4];
+            if constexpr (sizeof(T) == 4) {
+                v[0] = raw.v[c].x; v[1] = raw.v[c].y; v[2] = raw.v[c].z; v[3] = raw.v[c].w;
+            } else {
+                const u16x4 h = __builtin_bit_cast(u16x4, raw.v[c]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = (float)__builtin_bit_cast(T, (uint16_t)h[i]);
+            }
+            const int e0 = 4 * (q + LANES * c);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[4 * c + i] = e0 < E ? v[i] : -INFINITY;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) x[j] = q + LANES * j < E ? (float)raw.v[j] : -INFINITY;
+    }
+}
+template <bool AGAIN, typename T, int LANES, int VPL, bool VEC>
+__device__ __forceinline__ void row_values(const T *__restrict__ row, int E, int q, float (&x)[VPL])
+{
+    RowRaw<T, VPL, VEC> raw;
+    row_fetch<AGAIN, T, LANES, VPL, VEC>(row, E, q, raw);
+    row_take<T, LANES, VPL, VEC>(raw, E, q, x);
 }
 
 // The gradient of a row: written, or added to what is there.
@@ -146,7 +178,7 @@ __device__ __forceinline__ void row_store(T *__restrict__ row, int E, int q, boo
             const int e0 = 4 * (q + LANES * c);
             if (e0 < E) {
                 float v[4];
-                if (add) load4<false>(row + e0, v);
+                if (add) load4(row + e0, v);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[i] = add ? v[i] + x[4 * c + i] : x[4 * c + i];
                 store4(row + e0, v);
