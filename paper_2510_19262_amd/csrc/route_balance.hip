@@ -337,7 +337,7 @@ static Cut balance_cut(int64_t rows, int32_t groups, int E)
 {
     Cut c;
     int64_t few = 1;
-    by_shape(E, true, [&](auto s) { return (int)(few = 256 / decltype(s)::LANES); });
+    by_shape<true, float>(E, true, [&](auto s) { return (int)(few = 256 / decltype(s)::LANES); });
     for (c.threads = 256;; c.threads = 1024) {
         const int64_t in_hand = few * (c.threads / 256), rounds = rows / (2048 * 256 / c.threads * in_hand);
         c.slice_rows = (rounds > 1 ? rounds : 1) * in_hand;
@@ -415,7 +415,7 @@ extern "C" int railsched_route_balance(const void *logits, int32_t dtype, int64_
         const dim3 grid((unsigned)((rows + slice_rows - 1) / slice_rows));
         const int rc = by_dtype(dtype, [&](auto t) {
             using T = decltype(t);
-            return by_shape(E, in_fours<T>(logits, E, ld), [&](auto s) {
+            return by_shape<true, T>(E, in_fours<T>(logits, E, ld), [&](auto s) {
                 using S = decltype(s);
                 auto go = [&](auto threads, auto whole) {
                     hipLaunchKernelGGL((route_balance_kernel<T, S::LANES, S::VPL, S::VEC, decltype(threads)::value, decltype(whole)::value>), grid,
@@ -457,7 +457,7 @@ extern "C" int railsched_route_balance_backward(const void *logits, int32_t dtyp
     const Groups gr = make_groups(rows, group_off, groups);
     return by_dtype(dtype, [&](auto t) {
         using T = decltype(t);
-        return by_shape(E, in_fours<T>(logits, E, ld) && in_fours<T>(d_logits, E, ld_d), [&](auto s) {
+        return by_shape<true, T>(E, in_fours<T>(logits, E, ld) && in_fours<T>(d_logits, E, ld_d), [&](auto s) {
             using S = decltype(s);
             const int slice_rows = gradient_slice_rows(rows, (int)sizeof(T) * E, 256 / S::LANES);
             hipLaunchKernelGGL((route_balance_backward_kernel<T, S::LANES, S::VPL, S::VEC>), row_grid(rows, slice_rows), dim3(256), 0, st,

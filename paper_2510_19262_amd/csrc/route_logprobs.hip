@@ -232,7 +232,7 @@ extern "C" int railsched_route_logprobs(const void *logits, int32_t dtype, int64
             if (E <= 512) return go(Shape<16, 32, true>(), lists, std::integral_constant<int, 5>());
             return go(Shape<16, 64, true>(), lists, std::integral_constant<int, 5>());
         }
-        return by_shape(E, fours, [&](auto s) {
+        return by_shape<false, T>(E, fours, [&](auto s) {
             if (m > 0) return go(s, std::integral_constant<int, ALT_ROUNDS>(), std::integral_constant<int, 0>());
             return go(s, std::integral_constant<int, ALT_NONE>(), std::integral_constant<int, 0>());
         });
@@ -253,7 +253,7 @@ extern "C" int railsched_route_logprobs_backward(const void *logits, int32_t dty
     hipStream_t st = static_cast<hipStream_t>(stream);
     return by_dtype(dtype, [&](auto t) {
         using T = decltype(t);
-        return by_shape(E, in_fours<T>(logits, E, ld) && in_fours<T>(d_logits, E, ld_d), [&](auto s) {
+        return by_shape<true, T>(E, in_fours<T>(logits, E, ld) && in_fours<T>(d_logits, E, ld_d), [&](auto s) {
             using S = decltype(s);
             return launch_logprobs_backward<T, S::LANES, S::VPL, S::VEC, 1>(static_cast<const T *>(logits), rows, st, E, ld, 1.0f / temperature, row_mask,
                                                                             topk_idx, k, k > 0 ? d_logp : nullptr, d_lse, d_entropy, accumulate,

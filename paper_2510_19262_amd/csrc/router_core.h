@@ -361,32 +361,37 @@ struct Shape {
     static constexpr int LANES = L, VPL = V;
     static constexpr bool VEC = F;
 };
-// f(Shape) for rows of E logits.  The fewest lanes that leave at most 16 values to each (more would cost occupancy): every lane less is a step less in the
-// row's sums and more rows to a wavefront.  Rows that are read one by one have fewer shapes, as they are rare.
-template <typename F>
+// f(Shape) for rows of E logits.  Every lane less is a step less in the row's sums and more rows to a wavefront; more than 16 values a lane cost occupancy.
+// A kernel that only reads its rows (not WHOLE) takes the fewest lanes that pay: 8 values a lane at least, 16 or 32 of the short types, whose four are
+// half as many bytes.  2^22 x 32: 123 us with 4 lanes, 172 with 8; 2^20 x 64 bf16: 44 with 4, 48 with 8, but fp32 68 and 61; 2^20 x 256 bf16: 118 with 8 lanes,
+// 128 with 16, fp32 205 and 198.  One that writes them too, or keeps sums of its places (WHOLE), is faster with more: gradient of 2^22 x 32: 222 us
+// with 8 lanes, 247 with 4; 2^20 x 64: 95 with 8, 116 with 4.  Rows that are read one by one have fewer shapes, as they are rare.
+template <bool WHOLE, typename T, typename F>
 inline int by_shape(int E, bool fours, F f)
 {
+    constexpr bool brief = !WHOLE && sizeof(T) == 2;
     if (!fours) {
         if (E <= 16) return f(Shape<4, 4, false>());
         if (E <= 64) return f(Shape<8, 8, false>());
         if (E <= 256) return f(Shape<16, 16, false>());
         return f(Shape<64, 16, false>());
     }
-    if (E <= 8) return f(Shape<2, 4, true>());
-    if (E <= 16) return f(Shape<4, 4, true>());
-    if (E <= 32) return f(Shape<8, 4, true>());
-    if (E <= 64) return f(Shape<8, 8, true>());
+    if (E <= 8) return f(Shape<WHOLE ? 2 : 1, WHOLE ? 4 : 8, true>());
+    if (E <= 16) return f(Shape<WHOLE ? 4 : 2, WHOLE ? 4 : 8, true>());
+    if (E <= 32) return f(Shape<WHOLE ? 8 : 4, WHOLE ? 4 : 8, true>());
+    if (E <= 64) return f(Shape<brief ? 4 : 8, brief ? 16 : 8, true>());
     if (E <= 128) return f(Shape<8, 16, true>());
-    if (E <= 256) return f(Shape<16, 16, true>());
-    if (E <= 512) return f(Shape<32, 16, true>());
+    if (E <= 256) return f(Shape<brief ? 8 : 16, brief ? 32 : 16, true>());
+    if (E <= 512) return f(Shape<brief ? 16 : 32, brief ? 32 : 16, true>());
     return f(Shape<64, 16, true>());
 }
-// f(how many of `count` <= kMaxListed entries of a list a lane holds, at most): 1 where they fit, or as many as the longest list takes (of E entries at most)
+// f(how many of `count` <= kMaxListed entries of a list a lane holds, at most): 1 or 2 where they fit, or as many as the longest list takes (of E entries at most)
 template <typename S, typename F>
 inline int by_entries(int count, F f)
 {
     constexpr int most = S::VPL < kMaxListed / S::LANES ? S::VPL : kMaxListed / S::LANES;
     if (most == 1 || count <= S::LANES) return f(std::integral_constant<int, 1>());
+    if (most == 2 || count <= 2 * S::LANES) return f(std::integral_constant<int, 2>());
     return f(std::integral_constant<int, most>());
 }
 
