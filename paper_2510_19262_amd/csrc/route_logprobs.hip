@@ -7,8 +7,8 @@
 
 namespace rs {
 
-// How the most likely experts of a row are found: not at all, one round over the row each, or by the lists of stage 1's kernels.
-enum { ALT_NONE = 0, ALT_ROUNDS = 1, ALT_LISTS = 2 };
+// How the most likely experts of a row are found: not at all, one round over the row each, or by stage 1's lists of 8 or 16.
+enum { ALT_NONE = 0, ALT_ROUNDS = 1, ALT_LISTS_8 = 8, ALT_LISTS_16 = 16 };
 
 template <int LANES>
 __device__ __forceinline__ int row_min(int v)
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(256) void route_logprobs_kernel(const T *__restrict
         if constexpr (ALT == ALT_ROUNDS) {
             row_rounds<LANES, VPL, VEC>(x, m, q, each);
         } else {
-            constexpr int KM = 8;
+            constexpr int KM = ALT;
             constexpr unsigned MASK = (unsigned)(LANES * VPL) - 1u;
             float4 v[VPL / 4];
 #pragma unroll
@@ -223,14 +223,22 @@ extern "C" int railsched_route_logprobs(const void *logits, int32_t dtype, int64
                 static_cast<const T *>(logits), rows, st, E, ld, 1.0f / temperature, row_mask, topk_idx, k, m, logp, lse, entropy, alt_idx, alt_logp);
         };
         const bool fours = in_fours<T>(logits, E, ld);
-        // up to eight alternatives of rows of more than 32 logits come from stage 1's lists, in the shapes and list lengths that it uses
+        // up to 16 alternatives come from stage 1's lists, in the shapes and list lengths that it uses or that leave a lane whose whole list is taken as rare; up to
+        // eight of rows of more than 32 logits, more of rows of more than 64 (2^20 x 256 with 16: 758 us by rounds, 383 so)
         if (fours && E > 32 && m > 0 && m <= 8) {
-            constexpr std::integral_constant<int, ALT_LISTS> lists;
+            constexpr std::integral_constant<int, ALT_LISTS_8> lists;
             if (E <= 64) return go(Shape<4, 16, true>(), lists, std::integral_constant<int, 8>());
             if (E <= 128) return go(Shape<8, 16, true>(), lists, std::integral_constant<int, 6>());
             if (E <= 256) return go(Shape<16, 16, true>(), lists, std::integral_constant<int, 5>());
             if (E <= 512) return go(Shape<16, 32, true>(), lists, std::integral_constant<int, 5>());
             return go(Shape<16, 64, true>(), lists, std::integral_constant<int, 5>());
+        }
+        if (fours && E > 64 && m > 8 && m <= 16) {
+            constexpr std::integral_constant<int, ALT_LISTS_16> lists;
+            if (E <= 128) return go(Shape<8, 16, true>(), lists, std::integral_constant<int, 8>());
+            if (E <= 256) return go(Shape<16, 16, true>(), lists, std::integral_constant<int, 7>());
+            if (E <= 512) return go(Shape<16, 32, true>(), lists, std::integral_constant<int, 7>());
+            return go(Shape<16, 64, true>(), lists, std::integral_constant<int, 7>());
         }
         return by_shape<false, T>(E, fours, [&](auto s) {
             if (m > 0) return go(s, std::integral_constant<int, ALT_ROUNDS>(), std::integral_constant<int, 0>());

@@ -68,7 +68,7 @@ def _delta(x, tau, *more):
 
 def _t(x, tau):
     top = np.where(np.isfinite(x), x, -np.inf).max(axis=1, keepdims=True)
-    return np.where(np.isfinite(x), (top - x) / tau, 0.0)
+    return np.where(np.isfinite(x), top - np.where(np.isfinite(x), x, 0.0), 0.0) / tau
 
 
 def _near(got, want, tol, what):
@@ -568,3 +568,89 @@ def test_refusals_on_the_device():
                 lambda: rs.route_balance(x, it, ws=torch.empty(16, dtype=torch.uint8, device=DEV))):
         with pytest.raises(rs.RailschedError):
             bad()
+
+
+# ------------------------------------------------------------------------------------------------ the ways through the kernels
+@pytest.mark.parametrize("E", [8, 12, 32, 36, 40, 64, 68, 100, 128, 132, 240, 256, 260, 511, 512, 516, 1000, 1024])
+@pytest.mark.parametrize("kind", ["few values", "neighbours", "bf16", "mostly out"])
+def test_alternatives_in_stage_1s_order(E, kind):
+    """Ties, values a step apart and experts that are out, in every way of finding the largest: the order is that of a stable sort."""
+    rng = np.random.default_rng(E)
+    T = 260
+    if kind == "few values":
+        x = rng.integers(-2, 3, size=(T, E)).astype(np.float32)
+        x[x == 0] *= -1                                     # -0 and +0 are equal
+    elif kind == "neighbours":
+        x = (np.float32(1.0) + rng.integers(0, 6, size=(T, E)) * np.float32(2.0 ** -23)).astype(np.float32)
+        x *= np.where(rng.random((T, 1)) < 0.5, np.float32(-1), np.float32(1))
+    elif kind == "bf16":
+        x = rng.normal(size=(T, E)).astype(np.float32)
+    else:
+        x = np.where(rng.random((T, E)) < 0.97, -np.inf, rng.normal(size=(T, E))).astype(np.float32)
+    xt = _dev(x)
+    if kind == "bf16":
+        xt = xt.to(torch.bfloat16)
+        x = xt.float().cpu().numpy()
+    order = np.argsort(-x, axis=1, kind="stable")
+    for m in sorted({1, min(E, 4), min(E, 8), min(E, 9), min(E, 16), min(E, 17), min(E, 64)}):
+        ai, al = rs.route_logprobs(xt, alternatives=m)[3:]
+        want = np.where(np.take_along_axis(x, order[:, :m], 1) == -np.inf, -1, order[:, :m])
+        np.testing.assert_array_equal(ai.cpu().numpy(), want, err_msg=f"{m} alternatives")
+        wa = R.logprobs(x.astype(float), np.zeros((T, 0), int), m)[4]
+        _near(al, wa, (10 * np.abs(x[np.isfinite(x)]).max() + 80 + 8) * U, f"{m} alternatives")
+
+
+def test_a_grid_of_two_dimensions():
+    """More workgroups than one dimension of a grid takes here: 2^28 rows of two logits."""
+    T = (1 << 28) + 100
+    x = torch.zeros((T, 2), dtype=torch.bfloat16, device=DEV)
+    x[-50:, 0] = 1.0
+    x[:50, 1] = 2.0
+    lse = rs.route_logprobs(x)[1]
+    grad = rs.route_logprobs_backward(x, d_lse=torch.ones(T, device=DEV))
+    spread = rs.route_balance_backward(x, 1, torch.tensor([[3, 1]], device=DEV), torch.tensor([4], device=DEV), torch.ones(1, device=DEV))
+    for part in (slice(0, 1000), slice((1 << 27) - 500, (1 << 27) + 500), slice(T - 1000, T)):
+        at = x[part].double().cpu().numpy()
+        _near(lse[part], R.softmax(at)[3], 200 * U, "lse")
+        want, size = R.logprobs_backward(at, np.zeros((1000, 0), int), np.zeros((1000, 0)), np.ones(1000), np.zeros(1000))
+        _gradient_near(grad[part], want, size, at, 1.0, torch.bfloat16, 0, 3 * _delta(at, 1.0), "gradient of lse")
+        want, size = R.balance_backward(at, 1, [(0, 1000)], 1.0, np.array([[3, 1]]), np.array([4]), np.ones(1))
+        _gradient_near(spread[part], want, size, at, 1.0, torch.bfloat16, 8, 3 * _delta(at, 1.0), "gradient of the balance loss")
+    counts, tokens, sums, loss = rs.route_balance(x, torch.zeros((T, 1), dtype=torch.int32, device=DEV))
+    assert int(tokens) == T and counts.tolist() == [[T, 0]] and abs(float(sums.double().sum()) / T - 1) < 1e-5
+
+
+@pytest.mark.parametrize("groups", [1, 3, 16, 512, 4096])
+@pytest.mark.parametrize("E,dtype", [(8, "fp32"), (60, "bf16"), (61, "fp32"), (256, "fp32"), (512, "fp16"), (1024, "bf16")])
+def test_balance_of_equal_groups(groups, E, dtype):
+    """Groups in a workgroup of their own, in slices, in slices of the larger workgroups, with one tile of columns and several."""
+    rng = np.random.default_rng(groups + E)
+    dtype = TYPES[dtype]
+    for each in sorted({1, 37, (1 << 16) // groups // max(1, E // 64) + 1}):
+        T, k = groups * each, 2
+        if T * E > 1 << 23:
+            continue
+        xt, x = _logits(rng, T, E, dtype)
+        it, idx = _picks(rng, T, E, k)
+        mt, mask = _mask(rng, T)
+        counts, tokens, sums, loss = rs.route_balance(xt, it, groups=groups, coef=1.0, row_mask=mt)
+        wc, wn, ws, wl = R.balance(x, idx, [(g * each, (g + 1) * each) for g in range(groups)], 1.0, mask)
+        np.testing.assert_array_equal(counts.cpu().numpy(), wc)
+        np.testing.assert_array_equal(tokens.cpu().numpy(), wn)
+        worst = _delta(x, 1.0).max() + each * U
+        _near(sums, ws, worst * ws + 2 * each * U, "prob_sum")
+        share = E / (k * np.maximum(wn, 1.0) ** 2) * wc.sum(axis=1)
+        _near(loss, wl, wl * (worst + 2 * U) + share * 2 * each * U, "loss")
+
+
+def test_a_dirty_workspace_and_one_for_two_calls():
+    rng = np.random.default_rng(13)
+    for T, E, groups in ((5000, 64, 5), (70_000, 256, 1), (40, 8, 4)):
+        xt, x = _logits(rng, T, E, torch.float32)
+        it, _ = _picks(rng, T, E, 4)
+        yt, _ = _logits(rng, T, E, torch.float32)
+        want = [v.clone() for v in rs.route_balance(xt, it, groups=groups)], [v.clone() for v in rs.route_balance(yt, it, groups=groups)]
+        ws = torch.full((rs.route_balance_workspace_bytes(T, groups, E),), 0xFF, dtype=torch.uint8, device=DEV)
+        got = rs.route_balance(xt, it, groups=groups, ws=ws), rs.route_balance(yt, it, groups=groups, ws=ws)     # in order on one stream
+        for a, b in zip(want, got):
+            assert all(torch.equal(u, v) for u, v in zip(a, b))
