@@ -513,24 +513,30 @@ DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 class _Rows:
     """Checks of the operators on a router's logits: tensors on one device, launches on that device's current stream."""
+    __slots__ = ("logits", "device", "dtype", "rows", "E", "head")
 
     def __init__(self, logits: torch.Tensor):
         if not logits.is_cuda:
             raise ValueError("logits must be a device tensor")
-        if logits.dtype not in DTYPES:
+        self.dtype = logits.dtype
+        code = DTYPES.get(self.dtype)
+        if code is None:
             raise ValueError(f"logits must be torch.float32, bfloat16 or float16, got {logits.dtype}")
-        self.device, self.dtype = logits.device, logits.dtype
-        self.rows, self.E, self.ld = self._strided(logits, "logits")
-        self.logits = logits
+        self.logits, self.device = logits, logits.device
+        self.rows, self.E, ld = self._strided(logits, "logits")
+        self.head = (logits.data_ptr(), code, self.rows, self.E, ld)        # how every entry point's arguments begin
 
     @staticmethod
     def _strided(t: torch.Tensor, name: str):
-        if t.dim() != 2:
+        shape = t.shape
+        if len(shape) != 2:
             raise ValueError(f"{name} must have two dimensions")
-        rows, E = t.shape
-        if E > 1 and t.stride(1) != 1:
+        rows, E = shape
+        ld, step = t.stride()
+        if step != 1 and E > 1:
             raise ValueError(f"the values of a row of {name} must be next to each other")
-        ld = t.stride(0) if rows > 1 else max(E, 1)
+        if rows <= 1:
+            ld = max(E, 1)
         if ld < E:
             raise ValueError(f"the rows of {name} must not overlap")
         return rows, E, ld
@@ -542,9 +548,6 @@ class _Rows:
         if t.dim() != 2:
             raise ValueError(f"{name} must have two dimensions")
         return t.shape[1]
-
-    def head(self):
-        return self.logits.data_ptr(), DTYPES[self.dtype], self.rows, self.E, self.ld
 
     def arg(self, t: Optional[torch.Tensor], dtype, shape, name: str):
         """The address of a contiguous tensor of this type and shape on the logits' device; None for None."""
@@ -561,19 +564,21 @@ class _Rows:
         raise ValueError(f"{name} must be contiguous")
 
     def mask(self, t: Optional[torch.Tensor]):
-        if t is not None and t.dtype == torch.bool:
+        if t is None:
+            return None
+        if t.dtype == torch.bool:
             t = t.view(torch.uint8)
         return self.arg(t, torch.uint8, (self.rows,), "row_mask")
 
     def new(self, shape, dtype=torch.float32):
-        return torch.empty(shape, dtype=dtype, device=self.device)
+        return self.logits.new_empty(shape, dtype=dtype)
 
     def gradient(self, out: Optional[torch.Tensor], accumulate: bool):
         """(d_logits, its address, its row stride)"""
         if out is None:
             if accumulate:
                 raise ValueError("accumulate needs `out`, the gradient to add to")
-            out = self.new((self.rows, self.E), self.dtype)
+            out = self.logits.new_empty((self.rows, self.E))
             return out, out.data_ptr(), max(self.E, 1)
         if out.device != self.device or out.dtype != self.dtype or out.shape != (self.rows, self.E):
             raise ValueError(f"out must be {self.dtype} of shape {(self.rows, self.E)} on {self.device}")
@@ -610,7 +615,7 @@ def route_logprobs(logits: torch.Tensor, topk_idx: Optional[torch.Tensor] = None
         to = (r.arg(logp, torch.float32, (r.rows, k), "logp"), r.arg(lse, torch.float32, (r.rows,), "lse"),
               r.arg(entropy, torch.float32, (r.rows,), "entropy"), r.arg(alt_idx, torch.int32, (r.rows, m), "alt_idx"),
               r.arg(alt_logp, torch.float32, (r.rows, m), "alt_logp"))
-    r.call("railsched_route_logprobs", *r.head(), temperature, r.mask(row_mask), r.arg(topk_idx, torch.int32, (r.rows, k), "topk_idx"), k, m, *to)
+    r.call("railsched_route_logprobs", *r.head, temperature, r.mask(row_mask), r.arg(topk_idx, torch.int32, (r.rows, k), "topk_idx"), k, m, *to)
     return out
 
 
@@ -621,7 +626,7 @@ def route_logprobs_backward(logits: torch.Tensor, topk_idx: Optional[torch.Tenso
     r = _Rows(logits)
     k = r.width(topk_idx, "topk_idx")
     out, to, ld_d = r.gradient(out, accumulate)
-    r.call("railsched_route_logprobs_backward", *r.head(), temperature, r.mask(row_mask), r.arg(topk_idx, torch.int32, (r.rows, k), "topk_idx"), k,
+    r.call("railsched_route_logprobs_backward", *r.head, temperature, r.mask(row_mask), r.arg(topk_idx, torch.int32, (r.rows, k), "topk_idx"), k,
            r.arg(d_logp, torch.float32, (r.rows, k), "d_logp"), r.arg(d_lse, torch.float32, (r.rows,), "d_lse"),
            r.arg(d_entropy, torch.float32, (r.rows,), "d_entropy"), int(accumulate), to, ld_d)
     return out
@@ -645,15 +650,17 @@ def route_balance(logits: torch.Tensor, topk_idx: torch.Tensor, groups: int = 1,
     The groups are `groups` equal parts of the rows, or with group_off (int64 offsets) the rows between neighbouring offsets."""
     r = _Rows(logits)
     n, off = _groups(r, groups, group_off)
+    k = r.width(topk_idx, "topk_idx")
     if out is None:
         out = (r.new((n, r.E), torch.int64), r.new(n, torch.int64), r.new((n, r.E)), r.new(n))
-    counts, tokens, prob_sum, loss = out
-    k = r.width(topk_idx, "topk_idx")
+        to = [t.data_ptr() for t in out]
+    else:
+        counts, tokens, prob_sum, loss = out
+        to = (r.arg(counts, torch.int64, (n, r.E), "counts"), r.arg(tokens, torch.int64, (n,), "tokens"),
+              r.arg(prob_sum, torch.float32, (n, r.E), "prob_sum"), r.arg(loss, torch.float32, (n,), "loss"))
     if ws is None:
         ws = _ws(route_balance_workspace_bytes(r.rows, n, r.E), r.device)
-    r.call("railsched_route_balance", *r.head(), r.mask(row_mask), r.arg(topk_idx, torch.int32, (r.rows, k), "topk_idx"), k, off, n, coef,
-           r.arg(counts, torch.int64, (n, r.E), "counts"), r.arg(tokens, torch.int64, (n,), "tokens"),
-           r.arg(prob_sum, torch.float32, (n, r.E), "prob_sum"), r.arg(loss, torch.float32, (n,), "loss"),
+    r.call("railsched_route_balance", *r.head, r.mask(row_mask), r.arg(topk_idx, torch.int32, (r.rows, k), "topk_idx"), k, off, n, coef, *to,
            r.arg(ws, torch.uint8, ws.shape, "ws"), ws.numel())
     return out
 
@@ -668,7 +675,7 @@ def route_balance_backward(logits: torch.Tensor, k: int, counts: torch.Tensor, t
     if out is None and off is not None and not accumulate:
         out = torch.zeros((r.rows, r.E), dtype=r.dtype, device=r.device)
     out, to, ld_d = r.gradient(out, accumulate)
-    r.call("railsched_route_balance_backward", *r.head(), r.mask(row_mask), k, off, n, coef, r.arg(counts, torch.int64, (n, r.E), "counts"),
+    r.call("railsched_route_balance_backward", *r.head, r.mask(row_mask), k, off, n, coef, r.arg(counts, torch.int64, (n, r.E), "counts"),
            r.arg(tokens, torch.int64, (n,), "tokens"), r.arg(d_loss, torch.float32, (n,), "d_loss"), int(accumulate), to, ld_d)
     return out
 
@@ -680,9 +687,11 @@ def route_distill(logits: torch.Tensor, teacher_idx: torch.Tensor, teacher_logit
     K = r.width(teacher_idx, "teacher_idx")
     if out is None:
         out = r.new(r.rows)
-    r.call("railsched_route_distill", *r.head(), temperature, r.mask(row_mask), r.arg(teacher_idx, torch.int32, (r.rows, K), "teacher_idx"),
+    else:
+        r.arg(out, torch.float32, (r.rows,), "out")
+    r.call("railsched_route_distill", *r.head, temperature, r.mask(row_mask), r.arg(teacher_idx, torch.int32, (r.rows, K), "teacher_idx"),
            r.arg(teacher_logits, torch.float32, (r.rows, K), "teacher_logits"), r.arg(teacher_lse, torch.float32, (r.rows,), "teacher_lse"), K,
-           r.arg(out, torch.float32, (r.rows,), "out"))
+           out.data_ptr())
     return out
 
 
@@ -693,7 +702,7 @@ def route_distill_backward(logits: torch.Tensor, teacher_idx: torch.Tensor, teac
     r = _Rows(logits)
     K = r.width(teacher_idx, "teacher_idx")
     out, to, ld_d = r.gradient(out, accumulate)
-    r.call("railsched_route_distill_backward", *r.head(), temperature, r.mask(row_mask),
+    r.call("railsched_route_distill_backward", *r.head, temperature, r.mask(row_mask),
            r.arg(teacher_idx, torch.int32, (r.rows, K), "teacher_idx"), r.arg(teacher_logits, torch.float32, (r.rows, K), "teacher_logits"),
            r.arg(teacher_lse, torch.float32, (r.rows,), "teacher_lse"), K, r.arg(d_loss, torch.float32, (r.rows,), "d_loss"),
            int(accumulate), to, ld_d)
