@@ -223,20 +223,21 @@ extern "C" int railsched_route_logprobs(const void *logits, int32_t dtype, int64
                 static_cast<const T *>(logits), rows, st, E, ld, 1.0f / temperature, row_mask, topk_idx, k, m, logp, lse, entropy, alt_idx, alt_logp);
         };
         const bool fours = in_fours<T>(logits, E, ld);
-        // up to 16 alternatives come from stage 1's lists, in the shapes and list lengths that it uses or that leave a lane whose whole list is taken as rare; up to
-        // eight of rows of more than 32 logits, more of rows of more than 64 (2^20 x 256 with 16: 758 us by rounds, 383 so)
+        // Up to 16 alternatives come from stage 1's lists, in lengths that leave a lane whose whole list is taken as rare: up to eight of rows of more than 32 logits,
+        // more of rows of more than 64 (2^20 x 256 with 16: 758 us by rounds, 332 so).  These kernels are bound by their instructions, most of which a row of fewer
+        // lanes shares among more rows: 2^20 x 256 with 8 takes 256 us with 8 lanes, 296 with 16; bf16 194 and 261; but 2^20 x 128 222 with 4, 149 with 8.
         if (fours && E > 32 && m > 0 && m <= 8) {
             constexpr std::integral_constant<int, ALT_LISTS_8> lists;
             if (E <= 64) return go(Shape<4, 16, true>(), lists, std::integral_constant<int, 8>());
             if (E <= 128) return go(Shape<8, 16, true>(), lists, std::integral_constant<int, 6>());
-            if (E <= 256) return go(Shape<16, 16, true>(), lists, std::integral_constant<int, 5>());
+            if (E <= 256) return go(Shape<8, 32, true>(), lists, std::integral_constant<int, 6>());
             if (E <= 512) return go(Shape<16, 32, true>(), lists, std::integral_constant<int, 5>());
             return go(Shape<16, 64, true>(), lists, std::integral_constant<int, 5>());
         }
         if (fours && E > 64 && m > 8 && m <= 16) {
             constexpr std::integral_constant<int, ALT_LISTS_16> lists;
             if (E <= 128) return go(Shape<8, 16, true>(), lists, std::integral_constant<int, 8>());
-            if (E <= 256) return go(Shape<16, 16, true>(), lists, std::integral_constant<int, 7>());
+            if (E <= 256) return go(Shape<8, 32, true>(), lists, std::integral_constant<int, 8>());
             if (E <= 512) return go(Shape<16, 32, true>(), lists, std::integral_constant<int, 7>());
             return go(Shape<16, 64, true>(), lists, std::integral_constant<int, 7>());
         }
