@@ -64,37 +64,43 @@ __device__ __forceinline__ void distill_row(const T *__restrict__ logits, int64_
     const int entry0 = at_row.slot * K;
     t_idx += first * K;
     t_logit += first * K;
-    float tl[NK], xl[NK];
+    // Everything is asked for before anything is waited for: the entries first, whose experts' logits are the next thing to ask for.  Entries that no lane
+    // has cost nothing: the condition is the same for every lane, and there is none where one or two entries a lane are all there are.
+    auto has = [&](int r) { return NK <= 2 || LANES * r < K; };
+    int at[NK];
+    float tl[NK];
 #pragma unroll
     for (int r = 0; r < NK; ++r) {
-        o.at[r] = -1;
+        at[r] = -1;
         tl[r] = -INFINITY;
-        if (LANES * r < K) {                             // the same for every lane: entries that no lane has cost nothing
+        if (has(r)) {
             const int j = q0 + LANES * r;
-            o.at[r] = t_idx[entry0 + (j < K ? j : 0)];
+            at[r] = t_idx[entry0 + (j < K ? j : 0)];
             tl[r] = t_logit[entry0 + (j < K ? j : 0)];
-            if (j >= K) o.at[r] = -1;
         }
     }
     const float teacher = t_lse ? t_lse[first + at_row.slot] : 0.0f;
-    row_values<true, T, LANES, VPL, VEC>(from, E, q0, o.y);
+    RowRaw<T, VPL, VEC> raw;
+    row_fetch<true, T, LANES, VPL, VEC>(from, E, q0, raw);
+    T listed[NK];
     float best = -INFINITY;
     bool any = false;
 #pragma unroll
     for (int r = 0; r < NK; ++r) {
-        xl[r] = 0.0f;
-        if (LANES * r < K) {
-            if (o.at[r] < 0 || o.at[r] >= E || tl[r] == -INFINITY) { o.at[r] = -1; tl[r] = -INFINITY; }
-            xl[r] = (float)from[o.at[r] < 0 ? 0 : o.at[r]];
-            best = fmaxf(best, tl[r]);
-            any |= o.at[r] >= 0;
-        }
+        const bool good = q0 + LANES * r < K && at[r] >= 0 && at[r] < E && tl[r] != -INFINITY;
+        o.at[r] = good ? at[r] : -1;
+        tl[r] = good ? tl[r] : -INFINITY;
+        listed[r] = T(0.0f);
+        if (has(r)) listed[r] = from[good ? at[r] : 0];
+        best = fmaxf(best, tl[r]);
+        any |= good;
     }
     o.listed = row_any<LANES>(any);
     lds_fill<LANES, VPL, VEC>(mine, q0, -1.0f);
     lds_order();
     lds_mark<LANES, NK>(mine, q0, K, o.at, o.again);
     const float c = inv_tau * kLog2e;
+    row_take<T, LANES, VPL, VEC>(raw, E, q0, o.y);
     o.soft = row_softmax<LANES, VPL>(o.y, o.e, c);
     const float scale = inverse(o.soft.total);
     const float lse = fmaf(o.soft.largest, inv_tau, kLn2 * log2_of(o.soft.total));
@@ -103,29 +109,30 @@ __device__ __forceinline__ void distill_row(const T *__restrict__ logits, int64_
     if (t_lse) {
         log_mass = teacher;
 #pragma unroll
-        for (int r = 0; r < NK; ++r) o.q[r] = LANES * r < K && o.at[r] >= 0 ? pow2(kLog2e * fmaf(tl[r], inv_tau, -log_mass)) : 0.0f;
+        for (int r = 0; r < NK; ++r) o.q[r] = has(r) && o.at[r] >= 0 ? pow2(kLog2e * fmaf(tl[r], inv_tau, -log_mass)) : 0.0f;
     } else {
         best = row_max<LANES>(best);
         float s = 0.0f;
 #pragma unroll
         for (int r = 0; r < NK; ++r) {
-            o.q[r] = LANES * r < K && o.at[r] >= 0 ? pow2(c * (tl[r] - best)) : 0.0f;
+            o.q[r] = has(r) && o.at[r] >= 0 ? pow2(c * (tl[r] - best)) : 0.0f;
             s += o.q[r];
         }
         s = row_sum<LANES>(s);
         log_mass = fmaf(best, inv_tau, kLn2 * log2_of(s));
         const float share = inverse(s);
 #pragma unroll
-        for (int r = 0; r < NK; ++r) o.q[r] = LANES * r < K && o.at[r] >= 0 ? o.q[r] * share : 0.0f;
+        for (int r = 0; r < NK; ++r) o.q[r] = has(r) && o.at[r] >= 0 ? o.q[r] * share : 0.0f;
     }
     const float shift = log_mass - lse;
     float mass = 0.0f, gap = 0.0f;
 #pragma unroll
     for (int r = 0; r < NK; ++r) {
         o.p[r] = o.d[r] = 0.0f;
-        if (LANES * r < K) {
-            o.p[r] = o.at[r] >= 0 ? pow2(o.soft.y(xl[r], c)) * scale : 0.0f;
-            o.d[r] = fmaf(xl[r] - tl[r], inv_tau, shift);
+        if (has(r)) {
+            const float x = (float)listed[r];
+            o.p[r] = o.at[r] >= 0 ? pow2(o.soft.y(x, c)) * scale : 0.0f;
+            o.d[r] = fmaf(x - tl[r], inv_tau, shift);
             mass += o.q[r];
             gap += o.q[r] - (o.again[r] ? 0.0f : o.p[r]);
         }
@@ -141,7 +148,7 @@ __device__ __forceinline__ void distill_row(const T *__restrict__ logits, int64_
 }
 
 template <typename T, int LANES, int VPL, bool VEC, int NK>
-__global__ __launch_bounds__(256) void route_distill_kernel(const T *__restrict__ logits, int64_t rows, int E, int64_t ld, float tau,
+__global__ __launch_bounds__(256) void route_distill_kernel(const T *__restrict__ logits, int64_t rows, int E, int64_t ld, float tau, float inv_tau,
                                                             const uint8_t *__restrict__ row_mask, const int32_t *__restrict__ t_idx,
                                                             const float *__restrict__ t_logit, const float *__restrict__ t_lse, int K,
                                                             float *__restrict__ loss)
@@ -150,7 +157,6 @@ __global__ __launch_bounds__(256) void route_distill_kernel(const T *__restrict_
     __shared__ __align__(16) float lds[ROWS_PER_BLOCK * LANES * VPL];
     const int q0 = threadIdx.x % LANES;
     float *mine = lds + threadIdx.x / LANES * (LANES * VPL);
-    const float inv_tau = 1.0f / tau;
     const int64_t first = first_row(ROWS_PER_BLOCK);
     if (first >= rows) return;
     const RowAt at_row = row_at(threadIdx.x / LANES, rows - first, row_mask, first);
@@ -159,7 +165,7 @@ __global__ __launch_bounds__(256) void route_distill_kernel(const T *__restrict_
     float terms = 0.0f, twice = 0.0f;
 #pragma unroll
     for (int r = 0; r < NK; ++r) {
-        if (LANES * r < K && o.at[r] >= 0) {
+        if (o.at[r] >= 0) {
             // q (e^d - 1 - d) where e^d does not carry it off, and p alone where q has vanished
             terms += o.q[r] == 0.0f ? o.p[r] : o.d[r] < 1.0f ? o.q[r] * exp_above(o.d[r]) : o.p[r] - o.q[r] - o.q[r] * o.d[r];
             if (o.again[r]) twice += o.p[r];
@@ -180,7 +186,7 @@ __global__ __launch_bounds__(256) void route_distill_kernel(const T *__restrict_
 }
 
 template <typename T, int LANES, int VPL, bool VEC, int NK>
-__global__ __launch_bounds__(256) void route_distill_backward_kernel(const T *__restrict__ logits, int64_t rows, int E, int64_t ld, float tau,
+__global__ __launch_bounds__(256) void route_distill_backward_kernel(const T *__restrict__ logits, int64_t rows, int E, int64_t ld, float tau, float inv_tau,
                                                                      const uint8_t *__restrict__ row_mask, const int32_t *__restrict__ t_idx,
                                                                      const float *__restrict__ t_logit, const float *__restrict__ t_lse, int K,
                                                                      const float *__restrict__ d_loss, int add, T *__restrict__ d_logits,
@@ -190,7 +196,6 @@ __global__ __launch_bounds__(256) void route_distill_backward_kernel(const T *__
     __shared__ __align__(16) float lds[ROWS_PER_BLOCK * LANES * VPL];
     const int q0 = threadIdx.x % LANES;
     float *mine = lds + threadIdx.x / LANES * (LANES * VPL);
-    const float inv_tau = 1.0f / tau;
     const int64_t first = first_row(ROWS_PER_BLOCK);
     if (first >= rows) return;
     const RowAt at_row = row_at(threadIdx.x / LANES, rows - first, row_mask, first);
@@ -242,7 +247,7 @@ extern "C" int railsched_route_distill(const void *logits, int32_t dtype, int64_
             using S = decltype(s);
             return by_entries<S>(K, [&](auto n) {
             hipLaunchKernelGGL((route_distill_kernel<T, S::LANES, S::VPL, S::VEC, decltype(n)::value>), row_grid(rows, 256 / S::LANES), dim3(256), 0, st,
-                                   static_cast<const T *>(logits), rows, E, ld, temperature, row_mask, t_idx, t_logit, t_lse, K, loss);
+                                   static_cast<const T *>(logits), rows, E, ld, temperature, 1.0f / temperature, row_mask, t_idx, t_logit, t_lse, K, loss);
                 return launch_status();
             });
         });
@@ -267,7 +272,7 @@ extern "C" int railsched_route_distill_backward(const void *logits, int32_t dtyp
             using S = decltype(s);
             return by_entries<S>(K, [&](auto n) {
             hipLaunchKernelGGL((route_distill_backward_kernel<T, S::LANES, S::VPL, S::VEC, decltype(n)::value>), row_grid(rows, 256 / S::LANES), dim3(256), 0, st,
-                                   static_cast<const T *>(logits), rows, E, ld, temperature, row_mask, t_idx, t_logit, t_lse, K, d_loss, accumulate,
+                                   static_cast<const T *>(logits), rows, E, ld, temperature, 1.0f / temperature, row_mask, t_idx, t_logit, t_lse, K, d_loss, accumulate,
                                    static_cast<T *>(d_logits), ld_d);
                 return launch_status();
             });

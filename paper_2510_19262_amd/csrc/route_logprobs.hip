@@ -62,13 +62,13 @@ __global__ __launch_bounds__(256) void route_logprobs_kernel(const T *__restrict
     const T *__restrict__ from = row_of(logits + first * ld, at_row.slot, ld);
     const int32_t *__restrict__ ask = topk_idx + first * k + at_row.slot * k;
     int pick = -1;
-    if (k > 0) {                                     // a lane's first pick is fetched with the row
-        pick = ask[q < k ? q : 0];
-        if (pick >= E) pick = -1;
-    }
+    if (k > 0) pick = ask[q < k ? q : 0];                // a lane's first pick is fetched with the row, its logit before the row is waited for
+    RowRaw<T, VPL, VEC> raw;
+    row_fetch<true, T, LANES, VPL, VEC>(from, E, q, raw);
+    pick = pick < E ? pick : -1;
+    const T picked = from[pick < 0 ? 0 : pick];
     float x[VPL], dot;
-    row_values<true, T, LANES, VPL, VEC>(from, E, q, x);
-    const float picked = (float)from[pick < 0 ? 0 : pick];
+    row_take<T, LANES, VPL, VEC>(raw, E, q, x);
     const RowSoft soft = row_sums<LANES, VPL>(x, c, dot);
     const bool counts = at_row.live && soft.total != 0.0f;
     const float log_total = log2_of(soft.total);
@@ -76,7 +76,7 @@ __global__ __launch_bounds__(256) void route_logprobs_kernel(const T *__restrict
         if (lse) lse[row] = counts ? fmaf(soft.largest, inv_tau, kLn2 * log_total) : 0.0f;
         if (entropy) entropy[row] = counts ? kLn2 * (log_total - dot * inverse(soft.total)) : 0.0f;
     }
-    if (there && q < k) logp[row * k + q] = counts && pick >= 0 ? kLn2 * (soft.y(picked, c) - log_total) : 0.0f;
+    if (there && q < k) logp[row * k + q] = counts && pick >= 0 ? kLn2 * (soft.y((float)picked, c) - log_total) : 0.0f;
     if (there) {
         for (int j = q + LANES; j < k; j += LANES) {
             const int at = ask[j];
@@ -138,28 +138,38 @@ __global__ __launch_bounds__(256) void route_logprobs_backward_kernel(const T *_
     const int64_t first = first_row(ROWS_PER_BLOCK);
     if (first >= rows) return;
     const RowAt at_row = row_at(threadIdx.x / LANES, rows - first, row_mask, first);
-    float y[VPL], e[VPL];
-    row_values<false, T, LANES, VPL, VEC>(row_of(logits + first * ld, at_row.slot, ld), E, q, y);
+    // NK entries a lane at a time; the first ones are asked for before the row, as they are waited for first
     const int64_t entry0 = first * k + at_row.slot * k;
+    int at[NK];
+    float g[NK];
+    auto entries = [&](int j0) {
+#pragma unroll
+        for (int r = 0; r < NK; ++r) {
+            const int j = j0 + q + LANES * r;
+            const int64_t entry = entry0 + (j < k ? j : 0);
+            at[r] = topk_idx[entry];
+            g[r] = d_logp[entry];
+        }
+    };
+    if (d_logp) entries(0);
     const float along = d_lse ? d_lse[first + at_row.slot] : 0.0f;
     const float spread = d_entropy ? kLn2 * d_entropy[first + at_row.slot] : 0.0f;
+    RowRaw<T, VPL, VEC> raw;
+    row_fetch<false, T, LANES, VPL, VEC>(row_of(logits + first * ld, at_row.slot, ld), E, q, raw);
 
     float dx[VPL], sum = 0.0f;
 #pragma unroll
     for (int j = 0; j < VPL; ++j) dx[j] = 0.0f;
     if (d_logp) {
-        for (int j0 = 0; j0 < k; j0 += LANES * NK) {             // NK entries a lane at a time
-            int at[NK];
+        for (int j0 = 0; j0 < k; j0 += LANES * NK) {
             bool again[NK];
-            float g[NK], part[VPL];
+            float part[VPL];
+            if (j0 > 0) entries(j0);
 #pragma unroll
             for (int r = 0; r < NK; ++r) {
-                const int j = j0 + q + LANES * r;
-                const int64_t entry = entry0 + (j < k ? j : 0);
-                at[r] = topk_idx[entry];
-                g[r] = d_logp[entry];
-                if (j >= k || at[r] >= E) at[r] = -1;
-                if (at[r] < 0) g[r] = 0.0f;
+                const bool good = j0 + q + LANES * r < k && at[r] >= 0 && at[r] < E;
+                at[r] = good ? at[r] : -1;
+                g[r] = good ? g[r] : 0.0f;
                 sum += g[r];
             }
             lds_fill<LANES, VPL, VEC>(mine, q, 0.0f);
@@ -173,6 +183,8 @@ __global__ __launch_bounds__(256) void route_logprobs_backward_kernel(const T *_
         }
         sum = row_sum<LANES>(sum);
     }
+    float y[VPL], e[VPL];
+    row_take<T, LANES, VPL, VEC>(raw, E, q, y);
     const RowSoft soft = row_softmax<LANES, VPL>(y, e, inv_tau * kLog2e);
     const bool counts = at_row.live && soft.total != 0.0f;
     const float scale = inverse(soft.total), pull = sum - along;
