@@ -4,7 +4,7 @@
 // probabilities of its rows (fp32, a lane its own experts) and counts its picks (LDS), and writes one record.  Slices and groups are both in
 // row order, so the part of group g in slice s can take the record s + g: no two parts share it.  A second kernel adds the records of a group up
 // in their order (fp64) and forms the loss.  No floating-point atomics: equal inputs give equal bits.
-#include "router_core.h"
+#include "router_core.hpp"
 
 namespace rs {
 

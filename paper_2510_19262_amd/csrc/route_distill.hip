@@ -7,7 +7,7 @@
 // The loss is formed as  sum_j (q log(q/p) - q + p) + rest + (sum of q and p outside these terms):  every term is >= 0 and of second order where
 // p is near q, so a student near its teacher keeps its loss to fp32's relative accuracy, where sum q (log q - log p) would be a difference of
 // larger terms.  With d = log p - log q:  q log(q/p) - q + p = q (e^d - 1 - d).
-#include "router_core.h"
+#include "router_core.hpp"
 
 namespace rs {
 

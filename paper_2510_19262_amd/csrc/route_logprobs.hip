@@ -3,7 +3,7 @@
 // One pass over a row, in powers of two: the largest logit, then total = sum 2^y and dot = sum 2^y y from the values in registers (y <= 0: relative to the
 // largest).  lse = largest / tau + ln 2 log2 total, entropy = ln 2 (log2 total - dot / total) (no cancellation: both terms are >= 0), and the picks' logits
 // are read again, from the cache.
-#include "router_core.h"
+#include "router_core.hpp"
 
 namespace rs {
 

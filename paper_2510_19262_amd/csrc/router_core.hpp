@@ -1,6 +1,7 @@
 // Device-side pieces of the operators on a router's logits (log probabilities, balance loss, distillation): rows of
 // E <= 1024 logits held in registers by LANES consecutive lanes, VPL values each, their softmax, and a row in LDS
-// through which values listed by expert (picks, a teacher's entries) reach the lanes that hold the experts.
+// through which values listed by expert (picks, a teacher's entries) reach the lanes that hold the experts.  Not one of the .h files, which the
+// kernels of the five stages share and the figures measured for them go by: none of those kernels includes it.
 #pragma once
 
 #include "topk_core.h"
