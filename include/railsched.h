@@ -307,7 +307,7 @@ int railsched_port_round_robin(const int64_t *chunk_off, const uint8_t *rail, in
  *   row_mask  [rows] uint8, NULL = all rows count.  A row whose entry is 0 (padding) does not count, and neither does a
  *             row whose logits are all -infinity: whatever a masked row holds enters nothing, its picks are not counted, its
  *             floating outputs and its gradient are 0, its alternatives -1.
- *   temperature  tau, within 2^-100 .. 2^100: z = logits / tau, p = softmax(z) over the row, lse = log sum exp z.
+ *   temperature  tau, within 2^-60 .. 2^60: z = logits / tau, p = softmax(z) over the row, lse = log sum exp z.
  *   d_logits  the gradient, type `dtype`, row r at d_logits + r*ld_d, ld_d >= E; not the same memory as logits.  Places
  *             between the rows are left as they are.  accumulate = 0: overwritten; 1: added to what is there (each
  *             sum rounded to `dtype`; rows that do not count are left as they are).
@@ -349,7 +349,8 @@ int railsched_route_logprobs_backward(const void *logits, int32_t dtype, int64_t
  *   tokens    [groups] int64: n                                                 (out)
  *   prob_sum  [groups][E] fp32: P_e                                             (out)
  *   loss      [groups] fp32                                                     (out)
- *   ws        railsched_route_balance_workspace_bytes(rows, groups, E) bytes, 256-byte aligned
+ *   ws        railsched_route_balance_workspace_bytes(rows, groups, E) bytes, 256-byte aligned (contents undefined before and after; calls
+ *             that can run at the same time, captured graphs among them, need one each)
  * Errors as above, also INVALID_ARG where group_off is NULL and rows is not a multiple of groups, groups < 0, k < 1. */
 size_t railsched_route_balance_workspace_bytes(int64_t rows, int32_t groups, int32_t E);
 int railsched_route_balance(const void *logits, int32_t dtype, int64_t rows, int32_t E, int64_t ld, const uint8_t *row_mask,
@@ -370,7 +371,7 @@ int railsched_route_balance_backward(const void *logits, int32_t dtype, int64_t 
  * with an index outside [0,E) or the logit -infinity is absent.  Its probabilities are
  *   without t_lse: q = softmax(t_logit / tau) over the list;
  *   with t_lse:    q = exp(t_logit / tau - t_lse), t_lse the teacher's log-sum-exp over all its experts at this temperature, and the
- *                  rest q_r = max(0, 1 - sum q) is held against p_r, the sum of p outside the list (left out where p_r is 0).
+ *                  rest q_r = max(0, 1 - sum q) is held against p_r, the sum of p outside the list (left out where p_r is 0: below 2^-126).
  *   loss[r] = tau^2 (sum_j q_j (log q_j - log p[t_idx[j]]) + q_r (log q_r - log p_r))
  * A row without entries has the loss 0 (also with t_lse).  +infinity where q_j > 0 meets an expert that is out.
  * An expert listed twice counts with the sum of its entries' terms.

@@ -26,17 +26,17 @@ __device__ __forceinline__ float exp_above(float d)
     return fabsf(d) < 0.5f ? s : pow2(d * kLog2e) - 1.0f - d;
 }
 // x - log(1 + x), x > -1, the same way: with w = x / (2 + x), log(1 + x) = 2 (w + w^3/3 + w^5/5 + ...) and x - 2 w = x w.  |x| < 1/2: w^2 < 1/9, next
-// term below 2^-26 of it
-__device__ __forceinline__ float above_log(float x)
+// term below 2^-26 of it.  Further off 1 + x is given, as x near -1 has lost it.
+__device__ __forceinline__ float above_log(float x, float one_more)
 {
-    const float w = x / (2.0f + x), v = w * w;
+    const float w = x * inverse(2.0f + x), v = w * w;
     float s = fmaf(v, 1.0f / 15, 1.0f / 13);
     s = fmaf(v, s, 1.0f / 11);
     s = fmaf(v, s, 1.0f / 9);
     s = fmaf(v, s, 1.0f / 7);
     s = fmaf(v, s, 1.0f / 5);
     s = fmaf(v, s, 1.0f / 3);
-    return fabsf(x) < 0.5f ? w * (x - 2.0f * v * s) : x - kLn2 * log2_of(1.0f + x);
+    return fabsf(x) < 0.5f ? w * (x - 2.0f * v * s) : x - kLn2 * log2_of(one_more);
 }
 
 // What both passes need of a row.
@@ -144,7 +144,7 @@ __device__ __forceinline__ void distill_row(const T *__restrict__ logits, int64_
 #pragma unroll
     for (int j = 0; j < VPL; ++j) outside += marks[j] < 0.0f ? o.e[j] : 0.0f;
     o.rest_p = row_sum<LANES>(outside) * scale;
-    o.rest_q = t_lse && o.rest_p > 0.0f ? fmaxf(1.0f - o.mass, 0.0f) : 0.0f;
+    o.rest_q = t_lse && o.rest_p >= 0x1p-126f ? fmaxf(1.0f - o.mass, 0.0f) : 0.0f;
 }
 
 template <typename T, int LANES, int VPL, bool VEC, int NK>
@@ -176,8 +176,8 @@ __global__ __launch_bounds__(256) void route_distill_kernel(const T *__restrict_
     // sum q + q_r - (sum of p over the entries and outside): p of an expert listed twice is in its terms twice
     float sum = terms - twice;
     if (t_lse && o.rest_q > 0.0f) {
-        const float apart = o.gap / o.rest_q;                        // p_r / q_r - 1
-        sum += o.rest_q * above_log(apart);
+        const float over = inverse(o.rest_q);
+        sum += o.rest_q * above_log(o.gap * over, o.rest_p * over);      // p_r / q_r - 1 and p_r / q_r
     } else {
         sum += o.rest_p + (o.mass - 1.0f);
     }

@@ -291,17 +291,18 @@ __device__ __forceinline__ void lds_values(const float *row, int q, float (&x)[V
     }
 }
 
-// Marks the places at[r] (-1: none) of this lane's entries q, q + LANES, ... of `count` in the row; on return again[r] says that another entry of the same
-// place holds it (of several entries with one place exactly one is not `again`).  The marked places hold values >= 0.
+// Marks the places at[r] (-1: none) of this lane's entries q, q + LANES, ... of `count` in the row, whose places hold nothing above 0; on return again[r] says that a
+// later entry of the same place holds it (of several entries with one place exactly the last is not `again`).  The marked places hold values above 0.
 template <int LANES, int N>
 __device__ __forceinline__ void lds_mark(float *row, int q, int count, const int (&at)[N], bool (&again)[N])
 {
+    auto mark = [&](int r) { return __float_as_int((float)(q + LANES * r + 1)); };       // positive floats are in order as integers too
 #pragma unroll
     for (int r = 0; r < N; ++r)
-        if (LANES * r < count && at[r] >= 0) row[at[r]] = (float)(q + LANES * r);
+        if (LANES * r < count && at[r] >= 0) atomicMax(reinterpret_cast<int *>(row + at[r]), mark(r));
     lds_order();
 #pragma unroll
-    for (int r = 0; r < N; ++r) again[r] = LANES * r < count && at[r] >= 0 && row[at[r]] != (float)(q + LANES * r);
+    for (int r = 0; r < N; ++r) again[r] = LANES * r < count && at[r] >= 0 && __float_as_int(row[at[r]]) != mark(r);
     lds_order();
 }
 
@@ -336,7 +337,7 @@ __device__ __forceinline__ void lds_put(float *row, int q, int count, const int 
 inline int check_router(const void *logits, int32_t dtype, int64_t rows, int32_t E, int64_t ld, float temperature)
 {
     if (dtype < RAILSCHED_F32 || dtype > RAILSCHED_F16 || rows < 0 || E < 1 || ld < E) return RAILSCHED_ERR_INVALID_ARG;
-    if (!(temperature >= 0x1p-100f) || !(temperature <= 0x1p100f)) return RAILSCHED_ERR_INVALID_ARG;
+    if (!(temperature >= 0x1p-60f) || !(temperature <= 0x1p60f)) return RAILSCHED_ERR_INVALID_ARG;
     if (E > kMaxExperts || rows > 0x7FFFFFFFll || ld > (int64_t(1) << 31)) return RAILSCHED_ERR_UNSUPPORTED;
     if (rows > 0 && !logits) return RAILSCHED_ERR_NULL_PTR;
     return RAILSCHED_OK;

@@ -345,6 +345,38 @@ def test_teacher_equal_to_the_student_costs_nothing():
             assert np.abs(loss - want).max() < tau * tau * (200 * U * near / tau + (200 * U) ** 2 + (0 if K < E else 4 * U * U)) + 1e-12
 
 
+@pytest.mark.parametrize("far", [5.0, 12.0, 16.0, 40.0, 80.0, 120.0])
+def test_a_student_sure_of_the_list_and_a_teacher_that_is_not(far):
+    """The rest of the student's probability down to nothing, against a rest of the teacher's: the logarithm of their ratio, not of a difference."""
+    rng = np.random.default_rng(6)
+    T, E, K = 64, 32, 4
+    x = rng.normal(size=(T, E)).astype(np.float32)
+    x[:, :K] += np.float32(far)
+    idx = np.tile(np.arange(K), (T, 1))
+    logit = rng.normal(size=(T, K)).astype(np.float32)
+    lse = (np.log(np.exp(logit.astype(float)).sum(axis=1)) + 0.4).astype(np.float32)
+    loss = rs.route_distill(_dev(x), _dev(idx.astype(np.int32)), _dev(logit), _dev(lse))
+    o = R.distill_terms(x.astype(float), idx, logit.astype(float), lse.astype(float))
+    assert (o["rest_q"] > 0.3).all()
+    want = R.distill(x.astype(float), idx, logit.astype(float), lse.astype(float))
+    none = o["rest_p"] < 2.0 ** -126                        # the rest is left out where fp32 has nothing to hold against it
+    if none.any():
+        o["rest_q"] = np.where(none, 0.0, o["rest_q"])
+        log_p = np.take_along_axis(o["z"], o["at"], 1) - o["lse"][:, None]
+        want = np.where(none, (o["q"] * (o["u"] - o["log_mass"][:, None] - log_p)).sum(axis=1), want)
+    near_border = np.abs(np.log2(np.maximum(o["rest_p"], 1e-300)) + 126) < 1e-3
+    assert not near_border.any()
+    # terms of up to 0.4 far and their relative errors of (10 Z + 2.5 far + 70) u
+    _near(loss, want, (1 + np.abs(want)) * (10 * np.abs(x).max() + 2.5 * far + 100) * U, "loss")
+    g = rs.route_distill_backward(_dev(x), _dev(idx.astype(np.int32)), _dev(logit), torch.ones(T, device=DEV), _dev(lse))
+    wd, size = R.distill_backward(x.astype(float), idx, logit.astype(float), np.ones(T), lse.astype(float))
+    assert bool(g.isfinite().all())
+    some = ~none
+    # outside the list q_r p_e / p_r: p_e and p_r each off by (10 Z + 2.5 far + 70) u of themselves, and what lies below fp32's normal range by all of it
+    tol = np.abs(size) * 3 * (10 * np.abs(x).max() + 2.5 * far + 100) * U + 2 * 2.0 ** -126 * (1 + 1 / np.maximum(o["rest_p"], 2.0 ** -126))[:, None]
+    _near(g[_dev(some)], wd[some], tol[some], "gradient")
+
+
 def test_no_rows_and_no_groups():
     x = torch.empty((0, 8), device=DEV)
     idx = torch.empty((0, 2), dtype=torch.int32, device=DEV)
@@ -485,25 +517,26 @@ def test_another_stream():
         assert torch.equal(a, b)
 
 
-def test_captured_and_replayed():
+@pytest.mark.parametrize("T,E,n", [(4096, 64, 4), (70_000, 256, 1), (1000, 8, 8)])
+def test_captured_and_replayed(T, E, n):
     """Two graphs with workspaces of their own, replayed in turn with eager work between them, on new inputs."""
-    x, it, teacher, mask = _inputs(4)
-    _everything(x, it, teacher, mask)
+    x, it, teacher, mask = _inputs(4, T, E)
+    _everything(x, it, teacher, mask, n)
     torch.cuda.synchronize()
     graphs = []
     for _ in range(2):
         g = torch.cuda.CUDAGraph()
         with torch.cuda.graph(g):
-            out = _everything(x, it, teacher, mask)
+            out = _everything(x, it, teacher, mask, n)
         graphs.append((g, out))
     for seed in (5, 6, 7):
-        y, jt, other, mask2 = _inputs(seed)
+        y, jt, other, mask2 = _inputs(seed, T, E)
         x.copy_(y)
         it.copy_(jt)
         for a, b in zip(teacher, other):
             a.copy_(b)
         mask.copy_(mask2)
-        want = _everything(x, it, teacher, mask)
+        want = _everything(x, it, teacher, mask, n)
         for g, out in graphs:
             g.replay()
             torch.cuda.synchronize()

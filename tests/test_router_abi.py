@@ -38,7 +38,7 @@ def test_heads(head, want):
     assert lib.railsched_route_distill_backward(A, dt, rows, E, ld, 1.0, None, B, D, None, 2, D, 0, B, big, None) == want
 
 
-@pytest.mark.parametrize("tau", [0.0, -1.0, NAN, INF])
+@pytest.mark.parametrize("tau", [0.0, -1.0, NAN, INF, 2.0 ** 61, 2.0 ** -61])
 def test_temperature(tau):
     lib = rs.load()
     assert lib.railsched_route_logprobs(A, 0, 4, 8, 8, tau, None, B, 2, 0, D, None, None, None, None, None) == -1
