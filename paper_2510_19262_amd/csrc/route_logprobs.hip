@@ -22,8 +22,8 @@ __device__ __forceinline__ int row_min(int v)
     return v;
 }
 
-// The m largest logits of the row, one round each: emit(sel, expert) in every lane of the row, INT_MAX once only -infinity is left (and NaN, which is never
-// taken).  The winners are taken out of x.
+// The m largest logits of the row, one round each: emit(sel, expert, logit) in every lane of the row, INT_MAX once only -infinity is left (and NaN, which is
+// never taken).  The winners are taken out of x.
 template <int LANES, int VPL, bool VEC, typename F>
 __device__ __forceinline__ void row_rounds(float (&x)[VPL], int m, int q, F emit)
 {
@@ -40,7 +40,7 @@ __device__ __forceinline__ void row_rounds(float (&x)[VPL], int m, int q, F emit
         const int gone = winner == mine ? slot : VPL;
 #pragma unroll
         for (int j = 0; j < VPL; ++j) x[j] = j == gone ? -INFINITY : x[j];
-        emit(sel, winner);
+        emit(sel, winner, best);
     }
 }
 
@@ -66,8 +66,22 @@ __global__ __launch_bounds__(256) void route_logprobs_kernel(const T *__restrict
     RowRaw<T, VPL, VEC> raw;
     row_fetch<true, T, LANES, VPL, VEC>(from, E, q, raw);
     pick = pick < E ? pick : -1;
-    const T picked = from[pick < 0 ? 0 : pick];
     float x[VPL], dot;
+    // The lists give experts, not logits: rows of up to 32 KiB a workgroup wait for them in LDS.  By the time they are known the row has left the L2: fetched again,
+    // eight alternatives of 2^20 x 256 cost half a GiB of reads on top of one.  The picks of such a kernel are taken from there too.
+    constexpr bool keep = ALT >= ALT_LISTS_8 && 256 * VPL * sizeof(T) <= 32768;
+    __shared__ __align__(16) T lds[keep ? 256 * VPL : 1];
+    T *mine = lds + (keep ? threadIdx.x / LANES * (LANES * VPL) : 0);
+    T picked;
+    if constexpr (keep) {
+#pragma unroll
+        for (int i = 0; i < VPL / 4; ++i) *reinterpret_cast<typename RowRaw<T, VPL, VEC>::four *>(mine + 4 * (q + LANES * i)) = raw.v[i];
+        lds_order();
+        picked = mine[pick < 0 ? 0 : pick];
+    } else {
+        picked = from[pick < 0 ? 0 : pick];
+    }
+    auto kept = [&](int at) { return keep ? mine[at] : from[at < E ? at : 0]; };
     row_take<T, LANES, VPL, VEC>(raw, E, q, x);
     const RowSoft soft = row_sums<LANES, VPL>(x, c, dot);
     const bool counts = at_row.live && soft.total != 0.0f;
@@ -85,14 +99,13 @@ __global__ __launch_bounds__(256) void route_logprobs_kernel(const T *__restrict
         }
     }
     if constexpr (ALT != ALT_NONE) {
-        auto put = [&](int sel, int at) {            // an alternative: its logit once more, from the cache
-            const float v = at < E ? (float)from[at] : -INFINITY;
-            const bool good = counts && v != -INFINITY;
+        auto put = [&](int sel, int at, float v) {
+            const bool good = counts && at < E && v != -INFINITY;
             alt_idx[row * m + sel] = good ? at : -1;
             alt_logp[row * m + sel] = good ? kLn2 * (soft.y(v, c) - log_total) : counts ? -INFINITY : 0.0f;
         };
-        auto each = [&](int sel, int at) {
-            if (there && q == sel % LANES) put(sel, at);
+        auto each = [&](int sel, int at, float v) {
+            if (there && q == sel % LANES) put(sel, at, v);
         };
         if constexpr (ALT == ALT_ROUNDS) {
             row_rounds<LANES, VPL, VEC>(x, m, q, each);
@@ -112,7 +125,8 @@ __global__ __launch_bounds__(256) void route_logprobs_kernel(const T *__restrict
                     unsigned sel = 0;
 #pragma unroll
                     for (int j = r * LANES; j < KM && j < (r + 1) * LANES; ++j) sel = j == q + r * LANES ? u[j] : sel;
-                    if (there && q + r * LANES < m) put(q + r * LANES, (int)key_index<MASK>(sel));
+                    const int at = (int)key_index<MASK>(sel);
+                    if (there && q + r * LANES < m) put(q + r * LANES, at, (float)kept(at));
                 }
             } else {
                 row_rounds<LANES, VPL, VEC>(x, m, q, each);
