@@ -1,11 +1,12 @@
 // Balance loss of groups of rows with the counts of picks per expert, and its gradient.
 //
-// The rows are cut into slices, a workgroup each.  A slice holds parts of one or several groups; for each part the workgroup adds up the
-// probabilities of its rows (fp32, a lane its own experts) and counts its picks (LDS), and writes one record.  Slices and groups are both in
-// row order, so the part of group g in slice s can take the record s + g: no two parts share it.  A second kernel adds the records of a group up
-// in their order (fp64) and forms the loss.  No floating-point atomics: equal inputs give equal bits.
+// A workgroup adds up the probabilities of a part of a group's rows (fp32, a lane its own experts), counts its picks (LDS) and writes one record; a second kernel
+// adds the records of a group up in their order (fp64) and forms the loss.  No floating-point atomics: equal inputs give equal bits.  Equal groups are dealt out, `per`
+// workgroups to a group, round after round, so that what is in flight lies together; with one workgroup to a group the outputs leave at once.  Rows of ragged groups
+// are cut into slices, a workgroup each, whose parts are of one group or several; slices and groups are both in row order, so the part of group g in slice s can take
+// the record s + g: no two parts share it.
 //
-// Bound by the reads of logits and picks (2^25 x 8 with 2 picks: 1.34 GB in 224 us, 6.0 TB/s; one group of 2^20 x 256: 181 us), where the rows are few by a chain of dependent
+// Bound by the reads of logits and picks (2^25 x 8 with 2 picks: 1.34 GB in 210 us, 6.4 TB/s; one group of 2^20 x 256: 181 us), where the rows are few by a chain of dependent
 // reads (offsets, rows, records: 13 and 5 us for 300 sequences of 65537 x 61).  The gradient reads and writes every logit: 2^20 x 256 in 341 us, 6.3 TB/s.
 #include "router_core.hpp"
 
@@ -67,7 +68,8 @@ struct Records {
     unsigned *tickets;
     double *dots;
     int64_t words;
-    __device__ __forceinline__ float *at(int64_t slice, int64_t group) const { return data + (slice + group) * words; }
+    int per;                // records of a group, one after the other; 0: of slices
+    __device__ __forceinline__ float *at(int64_t r, int64_t group) const { return data + (r + (per ? group * per : group)) * words; }
 };
 
 constexpr int kMaxGroups = 1 << 23;                     // a workgroup each, within the work-items that a grid counts
@@ -105,12 +107,12 @@ __device__ __forceinline__ float balance_loss(float coef, int E, int k, int64_t 
     return n ? (float)((double)coef * E / ((double)k * n * n) * dot) : 0.0f;
 }
 
-// DIRECT: every slice is a whole group, whose outputs leave from here.
-template <typename T, int LANES, int VPL, bool VEC, int THREADS, bool DIRECT>
+// EQUAL: groups of `each` rows, dealt out to `per` workgroups; otherwise slices of slice_rows.
+template <typename T, int LANES, int VPL, bool VEC, int THREADS, bool EQUAL>
 __global__ __launch_bounds__(THREADS) void route_balance_kernel(const T *__restrict__ logits, int E, int64_t ld, const uint8_t *__restrict__ row_mask,
-                                                            const int32_t *__restrict__ topk_idx, int k, Groups groups, int64_t slice_rows, float coef,
-                                                            Records records, int64_t *__restrict__ counts, int64_t *__restrict__ tokens,
-                                                            float *__restrict__ prob_sum, float *__restrict__ loss)
+                                                                const int32_t *__restrict__ topk_idx, int k, Groups groups, int64_t slice_rows,
+                                                                float coef, Records records, int64_t *__restrict__ counts,
+                                                                int64_t *__restrict__ tokens, float *__restrict__ prob_sum, float *__restrict__ loss)
 {
     constexpr int ROWS_PER_BLOCK = THREADS / LANES, WAVES = THREADS / 64;
     __shared__ float sums[WAVES][LANES * VPL];
@@ -118,17 +120,10 @@ __global__ __launch_bounds__(THREADS) void route_balance_kernel(const T *__restr
     __shared__ unsigned counted;
     __shared__ double part[WAVES];
     const int q = threadIdx.x % LANES, slot = threadIdx.x / LANES, wave = threadIdx.x >> 6;
-    const int64_t r0 = blockIdx.x * slice_rows;
-    const int64_t r1 = r0 + slice_rows < groups.rows ? r0 + slice_rows : groups.rows;
-    if constexpr (!DIRECT) {
-        for (int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x; i < groups.n; i += (int64_t)gridDim.x * THREADS) records.tickets[i] = 0;
-    }
-    for (GroupWalk walk(groups, groups.holding(r0)); walk.g < groups.n; walk.next(groups)) {
-        const int g = walk.g;
-        const int64_t gb = walk.begin(), ge = walk.end();
-        if (gb >= r1) break;
-        const int64_t lo = gb > r0 ? gb : r0, hi = ge < r1 ? ge : r1;
-        if (lo >= hi) continue;
+    for (int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x; i < groups.n; i += (int64_t)gridDim.x * THREADS) records.tickets[i] = 0;
+
+    // the rows lo, lo + 1, ... (as many as the workgroup has in hand), then those `step` further on, up to hi: a part of group g, whose r-th record this is
+    auto add_up = [&](int g, int64_t lo, int64_t hi, int64_t step, int64_t r) {
         for (int i = threadIdx.x; i < E; i += THREADS) picks[i] = 0;
         if (threadIdx.x == 0) counted = 0;
         __syncthreads();
@@ -136,7 +131,7 @@ __global__ __launch_bounds__(THREADS) void route_balance_kernel(const T *__restr
 #pragma unroll
         for (int j = 0; j < VPL; ++j) acc[j] = 0.0f;
         unsigned here = 0;
-        // the rows in hand, with a lane's first pick; the next ones are on their way while these are worked on (2^25 x 8: 224 us, 241 without; 2^20 x 256 bf16 116, 159)
+        // the rows in hand, with a lane's first pick; the next ones are on their way while these are worked on (2^20 x 256 bf16: 116 us, 159 without)
         RowAt at_next;
         RowRaw<T, VPL, VEC> raw;
         int pick_next;
@@ -145,13 +140,19 @@ __global__ __launch_bounds__(THREADS) void route_balance_kernel(const T *__restr
             pick_next = topk_idx[w * k + at_next.slot * k + (q < k ? q : 0)];
             row_fetch<false, T, LANES, VPL, VEC>(row_of(logits + w * ld, at_next.slot, ld), E, q, raw);
         };
-        fetch(lo);
-        for (int64_t w0 = lo; w0 < hi; w0 += ROWS_PER_BLOCK) {
+        // each group starts at another of its rounds: groups a power of two apart would have all their workgroups at the same memory channels (32 groups of 2^20 x 8: 210 us, 228
+        // from the first round on)
+        const int64_t turns = lo < hi ? (hi - lo + step - 1) / step : 0;
+        int64_t turn = g * turns / groups.n;
+        if (turns) fetch(lo + turn * step);
+        for (int64_t done = 0; done < turns; ++done) {
+            const int64_t w0 = lo + turn * step;
+            if (++turn == turns) turn = 0;
             const RowAt at_row = at_next;
             const int pick = pick_next;
             float t[VPL], e[VPL];
             row_take<T, LANES, VPL, VEC>(raw, E, q, t);
-            if (w0 + ROWS_PER_BLOCK < hi) fetch(w0 + ROWS_PER_BLOCK);
+            if (done + 1 < turns) fetch(lo + turn * step);
             const RowSoft soft = row_softmax<LANES, VPL>(t, e, kLog2e);
             const bool use = at_row.live && soft.total != 0.0f;
             const float scale = inverse(soft.total);
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(THREADS) void route_balance_kernel(const T *__restr
             for (int w = 1; w < WAVES; ++w) s += sums[w][i];
             return s;
         };
-        if constexpr (DIRECT) {
+        if (EQUAL && records.per == 1) {
             double dot = 0.0;
             for (int i = threadIdx.x; i < E; i += THREADS) {
                 const float s = wave_sums(i);
@@ -193,7 +194,7 @@ __global__ __launch_bounds__(THREADS) void route_balance_kernel(const T *__restr
                 loss[g] = balance_loss(coef, E, k, counted, dot);
             }
         } else {
-            float *rec = records.at(blockIdx.x, g);
+            float *rec = records.at(r, g);
             for (int i = threadIdx.x; i < E; i += THREADS) {
                 rec[i] = wave_sums(i);
                 reinterpret_cast<unsigned *>(rec)[E + i] = picks[i];
@@ -201,6 +202,20 @@ __global__ __launch_bounds__(THREADS) void route_balance_kernel(const T *__restr
             if (threadIdx.x == 0) reinterpret_cast<unsigned *>(rec)[2 * E] = counted;
         }
         __syncthreads();
+    };
+
+    if constexpr (EQUAL) {
+        const int g = (int)(blockIdx.x / (unsigned)records.per), r = (int)(blockIdx.x % (unsigned)records.per);
+        add_up(g, g * groups.each + (int64_t)r * ROWS_PER_BLOCK, (g + 1) * groups.each, (int64_t)records.per * ROWS_PER_BLOCK, r);
+    } else {
+        const int64_t r0 = blockIdx.x * slice_rows;
+        const int64_t r1 = r0 + slice_rows < groups.rows ? r0 + slice_rows : groups.rows;
+        for (GroupWalk walk(groups, groups.holding(r0)); walk.g < groups.n; walk.next(groups)) {
+            const int64_t gb = walk.begin(), ge = walk.end();
+            if (gb >= r1) break;
+            const int64_t lo = gb > r0 ? gb : r0, hi = ge < r1 ? ge : r1;
+            if (lo < hi) add_up(walk.g, lo, hi, ROWS_PER_BLOCK, blockIdx.x);
+        }
     }
 }
 
@@ -218,7 +233,8 @@ __global__ __launch_bounds__(THREADS) void route_balance_join_kernel(Records rec
     const int g = blockIdx.x, tiles = gridDim.y;
     const int col = threadIdx.x % kTile, line = threadIdx.x / kTile;
     const int64_t gb = groups.begin(g), ge = groups.begin(g + 1);
-    const int64_t s0 = gb / slice_rows, s1 = gb < ge ? (ge - 1) / slice_rows + 1 : s0;
+    const int64_t s0 = records.per ? 0 : gb / slice_rows;
+    const int64_t s1 = records.per ? records.per : gb < ge ? (ge - 1) / slice_rows + 1 : s0;
     double dot = 0.0, n = 0.0;
     for (int i0 = blockIdx.y * kTile; i0 < E; i0 += tiles * kTile) {
         const int i = i0 + col;
@@ -330,22 +346,31 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
     }
 }
 
-// How the rows are cut: whole rounds of the rows that a workgroup has in hand.  Workgroups of 256 threads, 2048 or some more of them, where the groups are short;
-// of 1024 threads, 512 or some more, where a group would have more than 16 records of the smaller ones, so that its records stay few.
+// How the rows are shared out, in whole rounds of the rows that a workgroup has in hand.  Workgroups of 256 threads, 2048 or some more of them, where the groups are short; of
+// 1024 threads, 512 or some more, where a group would have more than 16 records of the smaller ones, so that its records stay few.  Equal groups of at most 16384 logits
+// have a workgroup of 256 threads each: one launch.
 struct Cut {
-    int64_t slice_rows, slices;
-    int threads;
+    int threads, per;       // per: workgroups to a group; 0: slices
+    int64_t slice_rows, blocks, records;
 };
-static Cut balance_cut(int64_t rows, int32_t groups, int E)
+static Cut balance_cut(int64_t rows, int32_t groups, int E, bool equal)
 {
-    Cut c;
-    int64_t few = 1;
-    by_shape<true, float>(E, true, [&](auto s) { return (int)(few = 256 / decltype(s)::LANES); });
+    Cut c = {};
+    int few = 1;
+    by_shape<true, float>(E, true, [&](auto s) { return few = 256 / decltype(s)::LANES; });
     for (c.threads = 256;; c.threads = 1024) {
-        const int64_t in_hand = few * (c.threads / 256), rounds = rows / (2048 * 256 / c.threads * in_hand);
-        c.slice_rows = (rounds > 1 ? rounds : 1) * in_hand;
-        c.slices = (rows + c.slice_rows - 1) / c.slice_rows;
-        if (c.threads == 1024 || c.slices <= 16 * (int64_t)groups) return c;
+        const int64_t in_hand = few * (c.threads / 256), wanted = 2048 * 256 / c.threads;
+        if (equal) {
+            const int64_t each = rows / groups, rounds = (each + in_hand - 1) / in_hand, share = (wanted + groups - 1) / groups;
+            c.per = each * E <= 16384 ? 1 : (int)(rounds < share ? rounds : share);
+            c.blocks = c.records = (int64_t)groups * c.per;
+        } else {
+            const int64_t rounds = rows / (wanted * in_hand);
+            c.slice_rows = (rounds > 1 ? rounds : 1) * in_hand;
+            c.blocks = (rows + c.slice_rows - 1) / c.slice_rows;
+            c.records = c.blocks + groups;
+        }
+        if (c.threads == 1024 || c.blocks <= 16 * (int64_t)groups) return c;
     }
 }
 // Rows of a workgroup of the gradient: 16 KiB of logits, 32 KiB of rows of more than 256 bytes; whole rounds of the rows in hand; fewer where the GPU would not be full.  Much
@@ -360,9 +385,12 @@ static int gradient_slice_rows(int64_t rows, int row_bytes, int in_hand)
 }
 static int balance_tiles(int E) { return (E + kTile - 1) / kTile; }
 
+// enough for equal groups and for ragged ones
 static size_t records_bytes(int64_t rows, int32_t groups, int32_t E)
 {
-    return align_up((size_t)(balance_cut(rows, groups, E).slices + groups + 1) * (2 * (size_t)E + 1) * sizeof(float), 256);
+    const int64_t ragged = balance_cut(rows, groups, E, false).records;
+    const int64_t equal = groups > 0 && rows % groups == 0 ? balance_cut(rows, groups, E, true).records : 0;
+    return align_up((size_t)(ragged > equal ? ragged : equal) * (2 * (size_t)E + 1) * sizeof(float), 256);
 }
 static size_t tickets_bytes(int32_t groups) { return align_up((size_t)groups * sizeof(unsigned), 256); }
 
@@ -405,37 +433,35 @@ extern "C" int railsched_route_balance(const void *logits, int32_t dtype, int64_
     if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 != 0 || ws_bytes < railsched_route_balance_workspace_bytes(rows, groups, E)) return RAILSCHED_ERR_WORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const Groups gr = make_groups(rows, group_off, groups);
-    // equal groups of few rows: a workgroup each, one launch and no records
-    const bool direct = !group_off && rows > 0 && gr.each * E <= 16384;
-    const Cut cut = balance_cut(rows, groups, E);
-    const int64_t slice_rows = direct ? gr.each : cut.slice_rows;
+    const Cut cut = balance_cut(rows, groups, E, !group_off);
     Records records;
     records.data = static_cast<float *>(ws);
     records.words = 2 * (int64_t)E + 1;
+    records.per = rows > 0 ? cut.per : 0;
     records.tickets = reinterpret_cast<unsigned *>(static_cast<char *>(ws) + records_bytes(rows, groups, E));
     records.dots = reinterpret_cast<double *>(reinterpret_cast<char *>(records.tickets) + tickets_bytes(groups));
     if (rows > 0) {
-        const dim3 grid((unsigned)((rows + slice_rows - 1) / slice_rows));
         const int rc = by_dtype(dtype, [&](auto t) {
             using T = decltype(t);
             return by_shape<true, T>(E, in_fours<T>(logits, E, ld), [&](auto s) {
                 using S = decltype(s);
-                auto go = [&](auto threads, auto whole) {
-                    hipLaunchKernelGGL((route_balance_kernel<T, S::LANES, S::VPL, S::VEC, decltype(threads)::value, decltype(whole)::value>), grid,
-                                       dim3(decltype(threads)::value), 0, st, static_cast<const T *>(logits), E, ld, row_mask, topk_idx, k, gr, slice_rows,
-                                       coef, records, counts, tokens, prob_sum, loss);
+                auto go = [&](auto threads, auto equal) {
+                    hipLaunchKernelGGL((route_balance_kernel<T, S::LANES, S::VPL, S::VEC, decltype(threads)::value, decltype(equal)::value>),
+                                       dim3((unsigned)cut.blocks), dim3(decltype(threads)::value), 0, st, static_cast<const T *>(logits), E, ld, row_mask,
+                                       topk_idx, k, gr, cut.slice_rows, coef, records, counts, tokens, prob_sum, loss);
+                    return launch_status();
                 };
-                if (direct) go(std::integral_constant<int, 256>(), std::true_type());
-                else if (cut.threads == 256) go(std::integral_constant<int, 256>(), std::false_type());
-                else go(std::integral_constant<int, 1024>(), std::false_type());
-                return launch_status();
+                constexpr std::integral_constant<int, 256> small;
+                constexpr std::integral_constant<int, 1024> large;
+                if (cut.per) return cut.threads == 256 ? go(small, std::true_type()) : go(large, std::true_type());
+                return cut.threads == 256 ? go(small, std::false_type()) : go(large, std::false_type());
             });
         });
-        if (rc || direct) return rc;
+        if (rc || cut.per == 1) return rc;
     }
     // a workgroup for every tile of columns where a group has many records; otherwise one for the group
-    const int64_t each = cut.slices / groups;
-    if (each > 16)
+    const int64_t slice_rows = cut.slice_rows > 0 ? cut.slice_rows : 1;
+    if (cut.records / groups > 16)
         hipLaunchKernelGGL(route_balance_join_kernel<1024>, dim3((unsigned)groups, (unsigned)balance_tiles(E)), dim3(1024), 0, st, records, E, k, gr, slice_rows,
                            coef, counts, tokens, prob_sum, loss);
     else
