@@ -1,7 +1,8 @@
 """railsched: batched LPT rail spraying of MoE all-to-all traffic on one MI355X.
 
 Thin ctypes binding over librailsched.so (hand-written HIP kernels for gfx950).
-Every step of the path runs in those kernels; this package only marshals arguments.
+Every step of the path runs in those kernels, and so do the operators on a router's logits beside its first
+stage; this package only marshals arguments.
 """
 from .binding import (  # noqa: F401
     Topo, RailschedError, lib_path, load, version, strerror,
