@@ -687,3 +687,41 @@ def test_a_dirty_workspace_and_one_for_two_calls():
         got = rs.route_balance(xt, it, groups=groups, ws=ws), rs.route_balance(yt, it, groups=groups, ws=ws)     # in order on one stream
         for a, b in zip(want, got):
             assert all(torch.equal(u, v) for u, v in zip(a, b))
+
+
+def test_a_teacher_whose_mass_is_off():
+    """A log-sum-exp that is too small (the list alone exceeds it: no rest) or too large (a rest that is not the teacher's) is taken as it is given."""
+    rng = np.random.default_rng(14)
+    for E, K in ((64, 8), (61, 61), (256, 16)):
+        xt, x = _logits(rng, 300, E, torch.float32)
+        idx, logit, lse = _teacher(rng, x, K, True, 1.0)
+        for shift in (-3.0, -0.7, 0.7, 3.0):
+            given = (lse + np.float32(shift)).astype(np.float32)
+            args = _dev(idx.astype(np.int32)), _dev(logit)
+            loss = rs.route_distill(xt, *args, _dev(given))
+            want = R.distill(x, idx, logit.astype(float), given.astype(float))
+            # q up to e^3: its error, that of p and of the logarithms, each of (10 Z + 70) u, times what is added up
+            size = 1 + np.exp(-shift) * (10 + np.abs(shift))
+            _near(loss, want, 4 * size * (10 * max(np.abs(x).max(), np.abs(given).max()) + 110) * U, f"loss of {E}, {shift}")
+            g = rs.route_distill_backward(xt, *args, torch.ones(300, device=DEV), _dev(given))
+            wd, mag = R.distill_backward(x, idx, logit.astype(float), np.ones(300), given.astype(float))
+            o = R.distill_terms(x, idx, logit.astype(float), given.astype(float))
+            mag = mag + o["p"] * np.where(o["rest_q"] > 0, (o["mass"] + 1) / np.maximum(o["rest_p"], 1e-300), 0.0)[:, None]
+            _near(g, wd, 4 * mag * (10 * max(np.abs(x).max(), np.abs(given).max()) + 110) * U + 2.0 ** -126, f"gradient of {E}, {shift}")
+
+
+def test_two_streams_at_once():
+    """Calls that run at the same time on buffers of their own do not reach each other."""
+    a, b = _inputs(15, 60_000, 256), _inputs(16, 60_000, 60)
+    want = _everything(*a), _everything(*b)
+    torch.cuda.synchronize()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    got = [[], []]
+    for _ in range(4):
+        for i, args in enumerate((a, b)):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(_everything(*args))
+    torch.cuda.synchronize()
+    for w, runs in zip(want, got):
+        for r in runs:
+            assert all(torch.equal(u, v) for u, v in zip(w, r))
