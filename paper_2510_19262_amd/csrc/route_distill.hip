@@ -15,6 +15,18 @@
 
 namespace rs {
 
+// e^a for a few values, a <= 0 or near it: the product with log2 e is carried on to a second float, as its rounding alone is 2^-24 |a| of the result
+__device__ __forceinline__ float exp_of(float a)
+{
+    const float y = a * kLog2e, low = fmaf(a, 0x1.4ae0c0p-26f, fmaf(a, kLog2e, -y));
+    return pow2(y) * (fabsf(low) < 1.0f ? fmaf(low, kLn2, 1.0f) : 1.0f);      // NaN where a is infinite
+}
+// a - log v of a normal v = m 2^k: k log 2 goes off in two parts, the first of them without rounding, as its sum with log m would be rounded at k
+__device__ __forceinline__ float less_log(float a, float v)
+{
+    const float k = (float)__builtin_amdgcn_frexp_expf(v), m = __builtin_amdgcn_frexp_mantf(v);
+    return fmaf(k, -0x1.63p-1f, a) - fmaf(k, -0x1.bd0106p-13f, kLn2 * log2_of(m));
+}
 // e^d - 1 - d: a series near 0, where the difference cancels.  |d| < 1/2: d^2/2 (1 + d/3 (1 + d/4 (... (1 + d/10)))), next term below 2^-27 of it
 __device__ __forceinline__ float exp_above(float d)
 {
@@ -52,6 +64,7 @@ struct Distilled {
     bool again[NK];              // an entry whose expert another entry of the list names too
     float q[NK], p[NK];          // the teacher's and the student's probability
     float d[NK];                 // log p - log q
+    float less[NK];              // for the gradient: q - p as q (1 - e^d), which does not cancel where p is near q; q alone where p is another entry's
     float mass;                  // sum of q (1 without t_lse)
     float gap;                   // sum of q - p over the entries (p of every expert once): with a tail p_r - q_r
     float rest_q, rest_p;
@@ -59,7 +72,7 @@ struct Distilled {
 };
 
 // The row `at_row` of the rows from `first` on.
-template <typename T, int LANES, int VPL, bool VEC, int NK>
+template <bool GRAD, typename T, int LANES, int VPL, bool VEC, int NK>
 __device__ __forceinline__ void distill_row(const T *__restrict__ logits, int64_t first, const RowAt &at_row, int E, int64_t ld, float inv_tau,
                                             const int32_t *__restrict__ t_idx, const float *__restrict__ t_logit,
                                             const float *__restrict__ t_lse, int K, int q0, float *mine, Distilled<LANES, VPL, NK> &o)
@@ -100,20 +113,19 @@ __device__ __forceinline__ void distill_row(const T *__restrict__ logits, int64_
         any |= good;
     }
     o.listed = row_any<LANES>(any);
-    lds_fill<LANES, VPL, VEC>(mine, q0, -1.0f);
+    lds_fill<LANES, VPL, VEC>(mine, q0, -INFINITY);
     lds_order();
     lds_mark<LANES, NK>(mine, q0, K, o.at, o.again);
     const float c = inv_tau * kLog2e;
     row_take<T, LANES, VPL, VEC>(raw, E, q0, o.y);
     o.soft = row_softmax<LANES, VPL>(o.y, o.e, c);
     const float scale = inverse(o.soft.total);
-    const float lse = fmaf(o.soft.largest, inv_tau, kLn2 * log2_of(o.soft.total));
-    // q, and the logarithm of the teacher's total mass
-    float log_mass;
+    // q, and the teacher's log total mass less the student's
+    float shift;
     if (t_lse) {
-        log_mass = teacher;
+        shift = less_log(fmaf(-o.soft.largest, inv_tau, teacher), o.soft.total);
 #pragma unroll
-        for (int r = 0; r < NK; ++r) o.q[r] = has(r) && o.at[r] >= 0 ? pow2(kLog2e * fmaf(tl[r], inv_tau, -log_mass)) : 0.0f;
+        for (int r = 0; r < NK; ++r) o.q[r] = has(r) && o.at[r] >= 0 ? exp_of(fmaf(tl[r], inv_tau, -teacher)) : 0.0f;
     } else {
         best = row_max<LANES>(best);
         float s = 0.0f;
@@ -123,22 +135,26 @@ __device__ __forceinline__ void distill_row(const T *__restrict__ logits, int64_
             s += o.q[r];
         }
         s = row_sum<LANES>(s);
-        log_mass = fmaf(best, inv_tau, kLn2 * log2_of(s));
         const float share = inverse(s);
+        shift = fmaf(best - o.soft.largest, inv_tau, kLn2 * log2_of(s * scale));
 #pragma unroll
         for (int r = 0; r < NK; ++r) o.q[r] = has(r) && o.at[r] >= 0 ? o.q[r] * share : 0.0f;
     }
-    const float shift = log_mass - lse;
     float mass = 0.0f, gap = 0.0f;
 #pragma unroll
     for (int r = 0; r < NK; ++r) {
-        o.p[r] = o.d[r] = 0.0f;
+        o.p[r] = o.d[r] = o.less[r] = 0.0f;
         if (has(r)) {
             const float x = (float)listed[r];
             o.p[r] = o.at[r] >= 0 ? pow2(o.soft.y(x, c)) * scale : 0.0f;
             o.d[r] = fmaf(x - tl[r], inv_tau, shift);
             mass += o.q[r];
-            gap += o.q[r] - (o.again[r] ? 0.0f : o.p[r]);
+            float less = o.q[r] - (o.again[r] ? 0.0f : o.p[r]);
+            if (GRAD) {
+                if (!o.again[r] && fabsf(o.d[r]) < 0.5f) less = -o.q[r] * (exp_above(o.d[r]) + o.d[r]);
+                o.less[r] = less;
+            }
+            gap += less;
         }
     }
     o.mass = t_lse ? row_sum<LANES>(mass) : 1.0f;
@@ -165,7 +181,7 @@ __global__ __launch_bounds__(256) void route_distill_kernel(const T *__restrict_
     if (first >= rows) return;
     const RowAt at_row = row_at(threadIdx.x / LANES, rows - first, row_mask, first);
     Distilled<LANES, VPL, NK> o;
-    distill_row<T, LANES, VPL, VEC, NK>(logits, first, at_row, E, ld, inv_tau, t_idx, t_logit, t_lse, K, q0, mine, o);
+    distill_row<false, T, LANES, VPL, VEC, NK>(logits, first, at_row, E, ld, inv_tau, t_idx, t_logit, t_lse, K, q0, mine, o);
     float terms = 0.0f, twice = 0.0f;
 #pragma unroll
     for (int r = 0; r < NK; ++r) {
@@ -204,22 +220,25 @@ __global__ __launch_bounds__(256) void route_distill_backward_kernel(const T *__
     if (first >= rows) return;
     const RowAt at_row = row_at(threadIdx.x / LANES, rows - first, row_mask, first);
     Distilled<LANES, VPL, NK> o;
-    distill_row<T, LANES, VPL, VEC, NK>(logits, first, at_row, E, ld, inv_tau, t_idx, t_logit, t_lse, K, q0, mine, o);
+    distill_row<true, T, LANES, VPL, VEC, NK>(logits, first, at_row, E, ld, inv_tau, t_idx, t_logit, t_lse, K, q0, mine, o);
     const bool counts = at_row.live && o.soft.total != 0.0f;
     const float along = d_loss[first + at_row.slot];
     lds_order();
-    lds_put<LANES, NK>(mine, q0, K, o.at, o.again, o.q);
+    // sum q - (Q + q_r) p: where Q + q_r is not 1, the rest of p goes along
+    const float off = o.rest_q > 0.0f ? 0.0f : 1.0f - o.mass;
+#pragma unroll
+    for (int r = 0; r < NK; ++r) o.less[r] = o.again[r] ? o.less[r] : fmaf(o.p[r], off, o.less[r]);
+    lds_put<LANES, NK>(mine, q0, K, o.at, o.again, o.less);
     float listed[VPL];
     lds_values<LANES, VPL, VEC>(mine, q0, listed);
     lds_order();
     const float unit = tau * along;
     const float scale = inverse(o.soft.total);
-    const float inside = (o.mass + o.rest_q) * scale;
     // Q + q_r - q_r / p_r is (p_r - q_r) / p_r where sum q + q_r is 1
     const float outside = (o.rest_q > 0.0f ? o.gap / o.rest_p : o.mass) * scale;
 #pragma unroll
     for (int j = 0; j < VPL; ++j) {
-        const float g = listed[j] < 0.0f ? o.e[j] * outside : o.e[j] * inside - listed[j];
+        const float g = listed[j] == -INFINITY ? o.e[j] * outside : -listed[j];
         o.y[j] = counts && o.listed ? unit * g : 0.0f;
     }
     if (at_row.there && (counts || !add)) row_store<T, LANES, VPL, VEC>(d_logits + (first + threadIdx.x / LANES) * ld_d, E, q0, add != 0, o.y);
