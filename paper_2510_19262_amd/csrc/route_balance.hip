@@ -7,7 +7,7 @@
 // the record s + g: no two parts share it.
 //
 // Bound by the reads of logits and picks (2^25 x 8 with 2 picks: 1.34 GB in 210 us, 6.4 TB/s; one group of 2^20 x 256: 181 us), where the rows are few by a chain of dependent
-// reads (offsets, rows, records: 13 and 5 us for 300 sequences of 65537 x 61).  The gradient reads and writes every logit: 2^20 x 256 in 341 us, 6.3 TB/s.
+// reads (offsets, rows, records: 13 and 6 us for 300 sequences of 65537 x 61).  The gradient reads and writes every logit: 2^20 x 256 in 341 us, 6.3 TB/s.
 #include "router_core.hpp"
 
 namespace rs {

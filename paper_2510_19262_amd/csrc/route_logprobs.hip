@@ -4,7 +4,7 @@
 // largest).  lse = largest / tau + ln 2 log2 total, entropy = ln 2 (log2 total - dot / total) (no cancellation: both terms are >= 0), and the picks' logits
 // are read again, from the cache.  It has to read the logits and picks and to write 8 bytes a row, 4 a pick and 8 an alternative: fp32 rows are bound by that
 // (2^20 x 256 with 8 picks: 1.15 GB in 207 us, 5.6 TB/s; 2^20 x 64: 62 us), rows of the short types and alternatives by the instructions (2^20 x 256 bf16: 118 us for
-// 0.6 GB; fp32 with 8 alternatives 237 us for 1.22 GB).  The gradient reads and writes every logit: 2^23 x 8 116 us, 2^20 x 256 345, 6.3 TB/s.
+// 0.6 GB; fp32 with 8 alternatives 228 us for 1.22 GB).  The gradient reads and writes every logit: 2^23 x 8 116 us, 2^20 x 256 345, 6.3 TB/s.
 #include "router_core.hpp"
 
 namespace rs {
