@@ -73,12 +73,13 @@ struct Records {
 };
 
 constexpr int kMaxGroups = 1 << 23;                     // a workgroup each, within the work-items that a grid counts
-constexpr int kTile = 32;                               // columns that a workgroup of the joining kernel adds up
+constexpr int kTile = 32;                               // columns of a tile where a grid of them joins the records
 
 // v added up over the lanes that are a multiple of LANES away from this one, in all of them
 template <int LANES>
 __device__ __forceinline__ float rows_sum(float v)
 {
+    if constexpr (LANES <= 1) v += xlane<1>(v);
     if constexpr (LANES <= 2) v += xlane<2>(v);
     if constexpr (LANES <= 4) v += __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(v), 0x101F));     // lane ^ 4
     if constexpr (LANES <= 8) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xF, 0xF, false));   // row_ror:8, lane ^ 8
@@ -219,24 +220,25 @@ __global__ __launch_bounds__(THREADS) void route_balance_kernel(const T *__restr
     }
 }
 
-// Adds the records of a group up: a workgroup takes kTile columns at a time (all of them, or one tile in a grid of tiles), its threads rows of records.
+// Adds the records of a group up: a workgroup takes TILE columns at a time (all of them, or one tile in a grid of tiles), its threads rows of records.  TILE holds the
+// columns where the records are few: every tile is a round trip to memory (164 groups of 13 records of 891 experts: 28 us in tiles of 32 for a call's 89).
 // The last tile of a group to arrive forms the loss from the tiles' products, in the order of the tiles.
-template <int THREADS>
+template <int THREADS, int TILE>
 __global__ __launch_bounds__(THREADS) void route_balance_join_kernel(Records records, int E, int k, Groups groups, int64_t slice_rows, float coef,
                                                                      int64_t *__restrict__ counts, int64_t *__restrict__ tokens,
                                                                      float *__restrict__ prob_sum, float *__restrict__ loss)
 {
-    constexpr int LINES = THREADS / kTile;
-    __shared__ double sums[LINES][kTile];
-    __shared__ int64_t picks[LINES][kTile];
+    constexpr int LINES = THREADS / TILE;
+    __shared__ double sums[LINES][TILE];
+    __shared__ int64_t picks[LINES][TILE];
     __shared__ double part[THREADS / 64];
     const int g = blockIdx.x, tiles = gridDim.y;
-    const int col = threadIdx.x % kTile, line = threadIdx.x / kTile;
+    const int col = threadIdx.x % TILE, line = threadIdx.x / TILE;
     const int64_t gb = groups.begin(g), ge = groups.begin(g + 1);
     const int64_t s0 = records.per ? 0 : gb / slice_rows;
     const int64_t s1 = records.per ? records.per : gb < ge ? (ge - 1) / slice_rows + 1 : s0;
     double dot = 0.0, n = 0.0;
-    for (int i0 = blockIdx.y * kTile; i0 < E; i0 += tiles * kTile) {
+    for (int i0 = blockIdx.y * TILE; i0 < E; i0 += tiles * TILE) {
         const int i = i0 + col;
         double s = 0.0;
         int64_t c = 0;
@@ -346,31 +348,32 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
     }
 }
 
-// How the rows are shared out, in whole rounds of the rows that a workgroup has in hand.  Workgroups of 256 threads, 2048 or some more of them, where the groups are short; of
-// 1024 threads, 512 or some more, where a group would have more than 16 records of the smaller ones, so that its records stay few.  Equal groups of at most 16384 logits
-// have a workgroup of 256 threads each: one launch.
+// How the rows are shared out, in whole rounds of the rows that a workgroup has in hand.  At most as many workgroups as are resident at a time, as one more is another round for
+// all: of 256 threads where the groups are short, 8 on a CU with 4 values to a lane, 6 with 8, 5 with 16; of 512 threads, 3 or 2, where a group would have more than 8 records
+// of the smaller ones, so that its records stay few (289392 x 128 in 24 groups: 35 us with 504 workgroups, 44 with 528 of 1024 threads; 2^20 x 64 in 200 ragged
+// groups: 59 and 65; 200000 x 1000 in 150: 141, 155 of 256 threads).  Equal groups of at most 16384 logits have a workgroup of 256 threads each: one launch.
 struct Cut {
     int threads, per;       // per: workgroups to a group; 0: slices
     int64_t slice_rows, blocks, records;
 };
-static Cut balance_cut(int64_t rows, int32_t groups, int E, bool equal)
+static Cut balance_cut(int64_t rows, int32_t groups, int E, bool equal, bool fours)
 {
     Cut c = {};
-    int few = 1;
-    by_shape<true, float>(E, true, [&](auto s) { return few = 256 / decltype(s)::LANES; });
-    for (c.threads = 256;; c.threads = 1024) {
-        const int64_t in_hand = few * (c.threads / 256), wanted = 2048 * 256 / c.threads;
+    int few = 1, vpl = 1;
+    by_shape<true, float>(E, fours, [&](auto s) { vpl = decltype(s)::VPL; return few = 256 / decltype(s)::LANES; });
+    for (c.threads = 256;; c.threads = 512) {
+        const int64_t in_hand = few * (c.threads / 256), wanted = c.threads == 256 ? (vpl >= 16 ? 1280 : vpl >= 8 ? 1536 : 2048) : (vpl >= 16 ? 512 : 768);
         if (equal) {
-            const int64_t each = rows / groups, rounds = (each + in_hand - 1) / in_hand, share = (wanted + groups - 1) / groups;
+            const int64_t each = rows / groups, rounds = (each + in_hand - 1) / in_hand, share = wanted > groups ? wanted / groups : 1;
             c.per = each * E <= 16384 ? 1 : (int)(rounds < share ? rounds : share);
             c.blocks = c.records = (int64_t)groups * c.per;
         } else {
-            const int64_t rounds = rows / (wanted * in_hand);
+            const int64_t rounds = (rows + wanted * in_hand - 1) / (wanted * in_hand);
             c.slice_rows = (rounds > 1 ? rounds : 1) * in_hand;
             c.blocks = (rows + c.slice_rows - 1) / c.slice_rows;
             c.records = c.blocks + groups;
         }
-        if (c.threads == 1024 || c.blocks <= 16 * (int64_t)groups) return c;
+        if (c.threads == 512 || c.blocks <= 8 * (int64_t)groups) return c;
     }
 }
 // Rows of a workgroup of the gradient: 16 KiB of logits, 32 KiB of rows of more than 256 bytes; whole rounds of the rows in hand; fewer where the GPU would not be full.  Much
@@ -385,12 +388,17 @@ static int gradient_slice_rows(int64_t rows, int row_bytes, int in_hand)
 }
 static int balance_tiles(int E) { return (E + kTile - 1) / kTile; }
 
-// enough for equal groups and for ragged ones
+// enough for equal groups and for ragged ones, however the rows lie
 static size_t records_bytes(int64_t rows, int32_t groups, int32_t E)
 {
-    const int64_t ragged = balance_cut(rows, groups, E, false).records;
-    const int64_t equal = groups > 0 && rows % groups == 0 ? balance_cut(rows, groups, E, true).records : 0;
-    return align_up((size_t)(ragged > equal ? ragged : equal) * (2 * (size_t)E + 1) * sizeof(float), 256);
+    int64_t most = 0;
+    for (int fours = 0; fours < 2; ++fours) {
+        const int64_t ragged = balance_cut(rows, groups, E, false, fours != 0).records;
+        const int64_t equal = groups > 0 && rows % groups == 0 ? balance_cut(rows, groups, E, true, fours != 0).records : 0;
+        most = ragged > most ? ragged : most;
+        most = equal > most ? equal : most;
+    }
+    return align_up((size_t)most * (2 * (size_t)E + 1) * sizeof(float), 256);
 }
 static size_t tickets_bytes(int32_t groups) { return align_up((size_t)groups * sizeof(unsigned), 256); }
 
@@ -433,7 +441,7 @@ extern "C" int railsched_route_balance(const void *logits, int32_t dtype, int64_
     if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 != 0 || ws_bytes < railsched_route_balance_workspace_bytes(rows, groups, E)) return RAILSCHED_ERR_WORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const Groups gr = make_groups(rows, group_off, groups);
-    const Cut cut = balance_cut(rows, groups, E, !group_off);
+    const Cut cut = balance_cut(rows, groups, E, !group_off, by_dtype(dtype, [&](auto t) { return (int)in_fours<decltype(t)>(logits, E, ld); }) != 0);
     Records records;
     records.data = static_cast<float *>(ws);
     records.words = 2 * (int64_t)E + 1;
@@ -452,22 +460,28 @@ extern "C" int railsched_route_balance(const void *logits, int32_t dtype, int64_
                     return launch_status();
                 };
                 constexpr std::integral_constant<int, 256> small;
-                constexpr std::integral_constant<int, 1024> large;
+                constexpr std::integral_constant<int, 512> large;
                 if (cut.per) return cut.threads == 256 ? go(small, std::true_type()) : go(large, std::true_type());
                 return cut.threads == 256 ? go(small, std::false_type()) : go(large, std::false_type());
             });
         });
         if (rc || cut.per == 1) return rc;
     }
-    // a workgroup for every tile of columns where a group has many records; otherwise one for the group
+    // a workgroup for every tile of columns where a group has many records; otherwise one for the group, whose tile is all of them
     const int64_t slice_rows = cut.slice_rows > 0 ? cut.slice_rows : 1;
-    if (cut.records / groups > 16)
-        hipLaunchKernelGGL(route_balance_join_kernel<1024>, dim3((unsigned)groups, (unsigned)balance_tiles(E)), dim3(1024), 0, st, records, E, k, gr, slice_rows,
-                           coef, counts, tokens, prob_sum, loss);
-    else
-        hipLaunchKernelGGL(route_balance_join_kernel<256>, dim3((unsigned)groups), dim3(256), 0, st, records, E, k, gr, slice_rows, coef, counts, tokens,
-                           prob_sum, loss);
-    return launch_status();
+    auto join = [&](auto threads, auto tile, unsigned tiles) {
+        hipLaunchKernelGGL((route_balance_join_kernel<decltype(threads)::value, decltype(tile)::value>), dim3((unsigned)groups, tiles), dim3(decltype(threads)::value),
+                           0, st, records, E, k, gr, slice_rows, coef, counts, tokens, prob_sum, loss);
+        return launch_status();
+    };
+    constexpr std::integral_constant<int, 64> narrow;
+    constexpr std::integral_constant<int, 256> small;
+    constexpr std::integral_constant<int, 1024> large;
+    if (cut.records / groups > 16) return join(large, std::integral_constant<int, kTile>(), (unsigned)balance_tiles(E));
+    if (E <= kTile) return join(small, std::integral_constant<int, kTile>(), 1);
+    if (E <= 64) return join(small, narrow, 1);
+    if (E <= 256) return join(small, small, 1);
+    return join(large, large, 1);
 }
 
 extern "C" int railsched_route_balance_backward(const void *logits, int32_t dtype, int64_t rows, int32_t E, int64_t ld, const uint8_t *row_mask,

@@ -368,12 +368,15 @@ struct Shape {
 // half as many bytes.  2^22 x 32: 123 us with 4 lanes, 172 with 8; 2^20 x 64 bf16: 44 with 4, 48 with 8, but fp32 68 and 61; 2^20 x 256 bf16: 118 with 8 lanes,
 // 128 with 16, fp32 205 and 198.  One that writes them too, or keeps sums of its places (WHOLE), is faster with more: gradient of 2^22 x 32: 222 us
 // with 8 lanes, 247 with 4; 2^20 x 64: 95 with 8, 116 with 4.  Rows that are read one by one (a width or a stride that is no multiple of four, an unaligned start) take
-// longer strips of neighbouring lanes: gradient of 2^20 x 61: 119 us with 16 lanes, 151 with 8, but read only 89 and 62.
+// longer strips of neighbouring lanes: gradient of 2^20 x 61: 119 us with 16 lanes, 151 with 8, but read only 89 and 62; up to 8 experts fit in one lane or two (gradient of
+// 25 2^20 x 2: 113 us with one lane, 258 with four; log probabilities of 5 2^20 x 7: 68 with two, 104).
 template <bool WHOLE, typename T, typename F>
 inline int by_shape(int E, bool fours, F f)
 {
     constexpr bool brief = !WHOLE && sizeof(T) == 2;
     if (!fours) {
+        if (E <= 4) return f(Shape<1, 4, false>());
+        if (E <= 8) return f(Shape<2, 4, false>());
         if (E <= 16) return f(Shape<4, 4, false>());
         if (E <= 32) return f(Shape<8, 4, false>());
         if (E <= 64) return f(Shape<WHOLE ? 16 : 8, WHOLE ? 4 : 8, false>());
