@@ -725,3 +725,25 @@ def test_two_streams_at_once():
     for w, runs in zip(want, got):
         for r in runs:
             assert all(torch.equal(u, v) for u, v in zip(w, r))
+
+
+@pytest.mark.parametrize("groups", [2, 20, 150, 1500])
+@pytest.mark.parametrize("E,dtype", [(2, "fp16"), (7, "fp32"), (33, "bf16"), (64, "fp32"), (100, "fp32"), (256, "bf16"), (300, "fp32"), (891, "fp16")])
+def test_balance_of_ragged_groups(groups, E, dtype):
+    """Groups cut into few and many records, whose columns are joined in one tile or several."""
+    rng = np.random.default_rng(groups * 3 + E)
+    dtype = TYPES[dtype]
+    T, k = min((1 << 23) // E, 400_000) - 5, 2
+    xt, x = _logits(rng, T, E, dtype)
+    it, idx = _picks(rng, T, E, k)
+    mt, mask = _mask(rng, T)
+    cuts = np.sort(rng.integers(0, T + 1, size=groups + 1))
+    counts, tokens, sums, loss = rs.route_balance(xt, it, group_off=_dev(cuts), coef=1.0, row_mask=mt)
+    wc, wn, ws, wl = R.balance(x, idx, list(zip(cuts[:-1], cuts[1:])), 1.0, mask)
+    np.testing.assert_array_equal(counts.cpu().numpy(), wc)
+    np.testing.assert_array_equal(tokens.cpu().numpy(), wn)
+    # as for the groups above: a group's sum is off by its terms, and by as many additions in fp32 as it has rows at most
+    worst = _delta(x, 1.0).max() + wn[:, None] * U
+    _near(sums, ws, worst * ws + 2 * wn[:, None] * U, "prob_sum")
+    share = E / (k * np.maximum(wn, 1.0) ** 2) * wc.sum(axis=1)
+    _near(loss, wl, wl * (worst[:, 0] + 2 * U) + share * 2 * wn * U, "loss")
