@@ -266,7 +266,7 @@ extern "C" int railsched_route_distill(const void *logits, int32_t dtype, int64_
     hipStream_t st = static_cast<hipStream_t>(stream);
     return by_dtype(dtype, [&](auto t) {
         using T = decltype(t);
-        return by_shape<false, T>(E, in_fours<T>(logits, E, ld), [&](auto s) {
+        return by_shape<false, T>(E, [&](auto s) {
             using S = decltype(s);
             return by_entries<S>(K, [&](auto n) {
             hipLaunchKernelGGL((route_distill_kernel<T, S::LANES, S::VPL, S::VEC, decltype(n)::value>), row_grid(rows, 256 / S::LANES), dim3(256), 0, st,
@@ -291,7 +291,7 @@ extern "C" int railsched_route_distill_backward(const void *logits, int32_t dtyp
     hipStream_t st = static_cast<hipStream_t>(stream);
     return by_dtype(dtype, [&](auto t) {
         using T = decltype(t);
-        return by_shape<true, T>(E, in_fours<T>(logits, E, ld) && in_fours<T>(d_logits, E, ld_d), [&](auto s) {
+        return by_shape<true, T>(E, [&](auto s) {
             using S = decltype(s);
             return by_entries<S>(K, [&](auto n) {
             hipLaunchKernelGGL((route_distill_backward_kernel<T, S::LANES, S::VPL, S::VEC, decltype(n)::value>), row_grid(rows, 256 / S::LANES), dim3(256), 0, st,

@@ -74,16 +74,17 @@ __global__ __launch_bounds__(256) void route_logprobs_kernel(const T *__restrict
     constexpr bool keep = ALT >= ALT_LISTS_8 && 256 * VPL * sizeof(T) <= 32768;
     __shared__ __align__(16) T lds[keep ? 256 * VPL : 1];
     T *mine = lds + (keep ? threadIdx.x / LANES * (LANES * VPL) : 0);
+    auto kept_at = [&](int at) { return at < (E & ~3) || at >= E ? at : at + (-E & 3); };      // the last values, if they are no whole four, stand at its end
     T picked;
     if constexpr (keep) {
 #pragma unroll
         for (int i = 0; i < VPL / 4; ++i) *reinterpret_cast<typename RowRaw<T, VPL, VEC>::four *>(mine + 4 * (q + LANES * i)) = raw.v[i];
         lds_order();
-        picked = mine[pick < 0 ? 0 : pick];
+        picked = mine[kept_at(pick < 0 ? 0 : pick)];
     } else {
         picked = from[pick < 0 ? 0 : pick];
     }
-    auto kept = [&](int at) { return keep ? mine[at] : from[at < E ? at : 0]; };
+    auto kept = [&](int at) { return keep ? mine[kept_at(at)] : from[at < E ? at : 0]; };
     row_take<T, LANES, VPL, VEC>(raw, E, q, x);
     const RowSoft soft = row_sums<LANES, VPL>(x, c, dot);
     const bool counts = at_row.live && soft.total != 0.0f;
@@ -250,12 +251,11 @@ extern "C" int railsched_route_logprobs(const void *logits, int32_t dtype, int64
             return launch_logprobs<T, S::LANES, S::VPL, S::VEC, decltype(alt)::value, decltype(length)::value>(
                 static_cast<const T *>(logits), rows, st, E, ld, 1.0f / temperature, row_mask, topk_idx, k, m, logp, lse, entropy, alt_idx, alt_logp);
         };
-        const bool fours = in_fours<T>(logits, E, ld);
         // Up to 16 alternatives come from stage 1's lists, in lengths that leave a lane whose whole list is taken as rare: up to eight of rows of more than 32 logits,
         // more of rows of more than 64 (2^20 x 256 with 16: about 700 us by rounds, 302 so).  These kernels are bound by their instructions, most of which a row of
         // fewer lanes shares among more rows: 2^20 x 256 with 8 takes 237 us with 8 lanes, 254 with 16; bf16 185 and 240; but 2^20 x 128 with 4 lanes half as long again
         // as with 8.
-        if (fours && E > 32 && m > 0 && m <= 8) {
+        if (E > 32 && m > 0 && m <= 8) {
             constexpr std::integral_constant<int, ALT_LISTS_8> lists;
             if (E <= 64) return go(Shape<4, 16, true>(), lists, std::integral_constant<int, 8>());
             if (E <= 128) return go(Shape<8, 16, true>(), lists, std::integral_constant<int, 6>());
@@ -263,14 +263,14 @@ extern "C" int railsched_route_logprobs(const void *logits, int32_t dtype, int64
             if (E <= 512) return go(Shape<16, 32, true>(), lists, std::integral_constant<int, 5>());
             return go(Shape<16, 64, true>(), lists, std::integral_constant<int, 5>());
         }
-        if (fours && E > 64 && m > 8 && m <= 16) {
+        if (E > 64 && m > 8 && m <= 16) {
             constexpr std::integral_constant<int, ALT_LISTS_16> lists;
             if (E <= 128) return go(Shape<8, 16, true>(), lists, std::integral_constant<int, 8>());
             if (E <= 256) return go(Shape<8, 32, true>(), lists, std::integral_constant<int, 8>());
             if (E <= 512) return go(Shape<16, 32, true>(), lists, std::integral_constant<int, 7>());
             return go(Shape<16, 64, true>(), lists, std::integral_constant<int, 7>());
         }
-        return by_shape<false, T>(E, fours, [&](auto s) {
+        return by_shape<false, T>(E, [&](auto s) {
             if (m > 0) return go(s, std::integral_constant<int, ALT_ROUNDS>(), std::integral_constant<int, 0>());
             return go(s, std::integral_constant<int, ALT_NONE>(), std::integral_constant<int, 0>());
         });
@@ -291,7 +291,7 @@ extern "C" int railsched_route_logprobs_backward(const void *logits, int32_t dty
     hipStream_t st = static_cast<hipStream_t>(stream);
     return by_dtype(dtype, [&](auto t) {
         using T = decltype(t);
-        return by_shape<true, T>(E, in_fours<T>(logits, E, ld) && in_fours<T>(d_logits, E, ld_d), [&](auto s) {
+        return by_shape<true, T>(E, [&](auto s) {
             using S = decltype(s);
             return launch_logprobs_backward<T, S::LANES, S::VPL, S::VEC, 1>(static_cast<const T *>(logits), rows, st, E, ld, 1.0f / temperature, row_mask,
                                                                             topk_idx, k, k > 0 ? d_logp : nullptr, d_lse, d_entropy, accumulate,

@@ -17,31 +17,35 @@ typedef _Float16 f16_t;
 
 constexpr int kMaxListed = 64;     // alternatives of a row, entries of a teacher's list
 
-// ---- four consecutive values: 16 bytes of fp32, 8 of the short types
+// ---- four consecutive values: 16 bytes of fp32, 8 of the short types, which global memory gives and takes at any address that a value can have
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 template <typename T>
 __device__ __forceinline__ void load4(const T *p, float (&v)[4])
 {
     if constexpr (sizeof(T) == 4) {
-        const f32x4 x = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p));
+        const f32x4 x = __builtin_nontemporal_load(reinterpret_cast<const f32x4_any *>(p));
         v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
     } else {
-        const u16x4 x = __builtin_bit_cast(u16x4, __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(p)));
+        const u16x4 x = __builtin_bit_cast(u16x4, __builtin_nontemporal_load(reinterpret_cast<const u32x2_any *>(p)));
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = (float)__builtin_bit_cast(T, (uint16_t)x[i]);
     }
 }
-template <typename T>
+template <bool STREAMING, typename T>
 __device__ __forceinline__ void store4(T *p, const float (&v)[4])
 {
     if constexpr (sizeof(T) == 4) {
-        f32x4 x;
+        f32x4_any x;
         x.x = v[0]; x.y = v[1]; x.z = v[2]; x.w = v[3];
-        __builtin_nontemporal_store(x, reinterpret_cast<f32x4 *>(p));
+        if constexpr (STREAMING) __builtin_nontemporal_store(x, reinterpret_cast<f32x4_any *>(p));
+        else *reinterpret_cast<f32x4_any *>(p) = x;
     } else {
         u16x4 x;
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = __builtin_bit_cast(uint16_t, (T)v[i]);      // to nearest, ties to even
-        __builtin_nontemporal_store(__builtin_bit_cast(u32x2, x), reinterpret_cast<u32x2 *>(p));
+        if constexpr (STREAMING) __builtin_nontemporal_store(__builtin_bit_cast(u32x2_any, x), reinterpret_cast<u32x2_any *>(p));
+        else *reinterpret_cast<u32x2_any *>(p) = __builtin_bit_cast(u32x2_any, x);
     }
 }
 
@@ -114,9 +118,11 @@ __device__ __forceinline__ T *row_of(T *first, int slot, int64_t ld) { return fi
 template <typename T, int VPL, bool VEC>
 struct RowRaw {
     typedef typename std::conditional<sizeof(T) == 4, f32x4, u32x2>::type four;
+    typedef typename std::conditional<sizeof(T) == 4, f32x4_any, u32x2_any>::type four_any;
     typename std::conditional<VEC, four, T>::type v[VEC ? VPL / 4 : VPL];
 };
-// VEC: places of four consecutive experts, interleaved over the lanes, as slot_index() numbers them.  Streaming, but for rows some of whose logits are
+// VEC (E >= 4): places of four consecutive experts, interleaved over the lanes, as slot_index() numbers them.  Where E is no multiple of four, the row's last four values stand for
+// the part of a four that it ends with, and are moved to their places when they are taken.  Streaming, but for rows some of whose logits are
 // fetched again (AGAIN): those are to stay in the L2 until then.  Gradient of the distillation of 2^20 x 256: 417 us streaming, 368 so; of the balance
 // loss, which fetches nothing again: 423, 432.
 template <bool AGAIN, typename T, int LANES, int VPL, bool VEC>
@@ -126,7 +132,7 @@ __device__ __forceinline__ void row_fetch(const T *__restrict__ row, int E, int 
 #pragma unroll
         for (int c = 0; c < VPL / 4; ++c) {
             const int e0 = 4 * (q + LANES * c);
-            const auto *from = reinterpret_cast<const typename RowRaw<T, VPL, VEC>::four *>(row + (e0 < E ? e0 : 0));
+            const auto *from = reinterpret_cast<const typename RowRaw<T, VPL, VEC>::four_any *>(row + (e0 < E - 4 ? e0 : E - 4));
             raw.v[c] = AGAIN ? *from : __builtin_nontemporal_load(from);
         }
     } else {
@@ -137,52 +143,84 @@ __device__ __forceinline__ void row_fetch(const T *__restrict__ row, int E, int 
         }
     }
 }
-// the values; places behind the row are -infinity
-template <typename T, int LANES, int VPL, bool VEC>
+template <typename T, typename R>
+__device__ __forceinline__ void four_values(const R &raw, float (&v)[4])
+{
+    if constexpr (sizeof(T) == 4) {
+        v[0] = raw.x; v[1] = raw.y; v[2] = raw.z; v[3] = raw.w;
+    } else {
+        const u16x4 h = __builtin_bit_cast(u16x4, raw);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (float)__builtin_bit_cast(T, (uint16_t)h[i]);
+    }
+}
+// the values; places behind the row are -infinity.  PARTS: whether the row may end with a part of a four
+template <typename T, int LANES, int VPL, bool VEC, bool PARTS = true>
 __device__ __forceinline__ void row_take(const RowRaw<T, VPL, VEC> &raw, int E, int q, float (&x)[VPL])
 {
     if constexpr (VEC) {
+        float v[4];
 #pragma unroll
         for (int c = 0; c < VPL / 4; ++c) {
-            float v[4];
-            if constexpr (sizeof(T) == 4) {
-                v[0] = raw.v[c].x; v[1] = raw.v[c].y; v[2] = raw.v[c].z; v[3] = raw.v[c].w;
-            } else {
-                const u16x4 h = __builtin_bit_cast(u16x4, raw.v[c]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = (float)__builtin_bit_cast(T, (uint16_t)h[i]);
-            }
+            four_values<T>(raw.v[c], v);
             const int e0 = 4 * (q + LANES * c);
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[4 * c + i] = e0 < E ? v[i] : -INFINITY;
+        }
+        if (const int r = E & 3; PARTS && r != 0) {
+#pragma unroll
+            for (int c = 0; c < VPL / 4; ++c) {
+                if ((E >> 2) / LANES != c) continue;      // of these, a lane has the row's last r < 4 values
+                four_values<T>(raw.v[c], v);
+                const bool last = q == (E >> 2) % LANES;
+                x[4 * c] = last ? (r == 1 ? v[3] : r == 2 ? v[2] : v[1]) : x[4 * c];
+                x[4 * c + 1] = last ? (r == 1 ? -INFINITY : r == 2 ? v[3] : v[2]) : x[4 * c + 1];
+                x[4 * c + 2] = last ? (r == 3 ? v[3] : -INFINITY) : x[4 * c + 2];
+                x[4 * c + 3] = last ? -INFINITY : x[4 * c + 3];
+            }
         }
     } else {
 #pragma unroll
         for (int j = 0; j < VPL; ++j) x[j] = q + LANES * j < E ? (float)raw.v[j] : -INFINITY;
     }
 }
-template <bool AGAIN, typename T, int LANES, int VPL, bool VEC>
+template <bool AGAIN, typename T, int LANES, int VPL, bool VEC, bool PARTS = true>
 __device__ __forceinline__ void row_values(const T *__restrict__ row, int E, int q, float (&x)[VPL])
 {
     RowRaw<T, VPL, VEC> raw;
     row_fetch<AGAIN, T, LANES, VPL, VEC>(row, E, q, raw);
-    row_take<T, LANES, VPL, VEC>(raw, E, q, x);
+    row_take<T, LANES, VPL, VEC, PARTS>(raw, E, q, x);
 }
 
-// The gradient of a row: written, or added to what is there.
-template <typename T, int LANES, int VPL, bool VEC>
+// The gradient of a row: written, or added to what is there.  Streaming where its fours are all there is; a row that ends with a part of a four has lines written
+// by two stores, which then meet in the L2 (gradient of 2^20 x 61: 114 us, 243 streaming).
+template <typename T, int LANES, int VPL, bool VEC, bool PARTS = true>
 __device__ __forceinline__ void row_store(T *__restrict__ row, int E, int q, bool add, const float (&x)[VPL])
 {
     if constexpr (VEC) {
+        auto four = [&](int c, int e0, auto streaming) {
+            float v[4];
+            if (add) load4(row + e0, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = add ? v[i] + x[4 * c + i] : x[4 * c + i];
+            store4<decltype(streaming)::value>(row + e0, v);
+        };
+        if (!PARTS || (E & 3) == 0) {
+#pragma unroll
+            for (int c = 0; c < VPL / 4; ++c) {
+                const int e0 = 4 * (q + LANES * c);
+                if (e0 < E) four(c, e0, std::true_type());
+            }
+            return;
+        }
 #pragma unroll
         for (int c = 0; c < VPL / 4; ++c) {
             const int e0 = 4 * (q + LANES * c);
-            if (e0 < E) {
-                float v[4];
-                if (add) load4(row + e0, v);
+            if (e0 + 4 <= E) four(c, e0, std::false_type());
+            if ((E >> 2) / LANES == c && q == (E >> 2) % LANES) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = add ? v[i] + x[4 * c + i] : x[4 * c + i];
-                store4(row + e0, v);
+                for (int i = 0; i < 3; ++i)
+                    if (e0 + i < E) row[e0 + i] = (T)(add ? (float)row[e0 + i] + x[4 * c + i] : x[4 * c + i]);
             }
         }
     } else {
@@ -350,13 +388,6 @@ inline int check_gradient(const void *logits, const void *d_logits, int64_t rows
     if (rows > 0 && d_logits == logits) return RAILSCHED_ERR_INVALID_ARG;
     return RAILSCHED_OK;
 }
-// whether rows can be read or written four values at a time
-template <typename T>
-inline bool in_fours(const void *p, int32_t E, int64_t ld)
-{
-    return E % 4 == 0 && ld % 4 == 0 && reinterpret_cast<uintptr_t>(p) % (4 * sizeof(T)) == 0;
-}
-
 // The shape a row of E logits is held in: LANES lanes, VPL values each, in places of four or one by one.
 template <int L, int V, bool F>
 struct Shape {
@@ -367,23 +398,16 @@ struct Shape {
 // A kernel that only reads its rows (not WHOLE) takes the fewest lanes that pay: 8 values a lane at least, 16 or 32 of the short types, whose four are
 // half as many bytes.  2^22 x 32: 123 us with 4 lanes, 172 with 8; 2^20 x 64 bf16: 44 with 4, 48 with 8, but fp32 68 and 61; 2^20 x 256 bf16: 118 with 8 lanes,
 // 128 with 16, fp32 205 and 198.  One that writes them too, or keeps sums of its places (WHOLE), is faster with more: gradient of 2^22 x 32: 222 us
-// with 8 lanes, 247 with 4; 2^20 x 64: 95 with 8, 116 with 4.  Rows that are read one by one (a width or a stride that is no multiple of four, an unaligned start) take
-// longer strips of neighbouring lanes: gradient of 2^20 x 61: 119 us with 16 lanes, 151 with 8, but read only 89 and 62; up to 8 experts fit in one lane or two (gradient of
-// 25 2^20 x 2: 113 us with one lane, 258 with four; log probabilities of 5 2^20 x 7: 68 with two, 104).
+// with 8 lanes, 247 with 4; 2^20 x 64: 95 with 8, 116 with 4.  Read and written one by one: rows of less than four, and where WHOLE short ones that end with a part of a four (gradients
+// of 2^26 logits in rows of 11: 128 us, 142 in fours; of 27: 139 and 131, of 45 bf16: 133 and 88).
 template <bool WHOLE, typename T, typename F>
-inline int by_shape(int E, bool fours, F f)
+inline int by_shape(int E, F f)
 {
     constexpr bool brief = !WHOLE && sizeof(T) == 2;
-    if (!fours) {
-        if (E <= 4) return f(Shape<1, 4, false>());
-        if (E <= 8) return f(Shape<2, 4, false>());
-        if (E <= 16) return f(Shape<4, 4, false>());
-        if (E <= 32) return f(Shape<8, 4, false>());
-        if (E <= 64) return f(Shape<WHOLE ? 16 : 8, WHOLE ? 4 : 8, false>());
-        if (E <= 128) return f(Shape<16, 8, false>());
-        if (E <= 256) return f(Shape<WHOLE ? 32 : 16, WHOLE ? 8 : 16, false>());
-        if (E <= 512) return f(Shape<WHOLE ? 64 : 32, WHOLE ? 8 : 16, false>());
-        return f(Shape<64, 16, false>());
+    if (E < 4) return f(Shape<1, 4, false>());
+    if constexpr (WHOLE) {
+        if (E > 8 && E <= 16 && E % 4 != 0) return f(Shape<4, 4, false>());
+        if (E > 16 && E <= 32 && E % 4 != 0) return f(Shape<8, 4, false>());
     }
     if (E <= 8) return f(Shape<WHOLE ? 2 : 1, WHOLE ? 4 : 8, true>());
     if (E <= 16) return f(Shape<WHOLE ? 4 : 2, WHOLE ? 4 : 8, true>());

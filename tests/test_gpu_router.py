@@ -747,3 +747,48 @@ def test_balance_of_ragged_groups(groups, E, dtype):
     _near(sums, ws, worst * ws + 2 * wn[:, None] * U, "prob_sum")
     share = E / (k * np.maximum(wn, 1.0) ** 2) * wc.sum(axis=1)
     _near(loss, wl, wl * (worst[:, 0] + 2 * U) + share * 2 * wn * U, "loss")
+
+
+@pytest.mark.parametrize("E", [5, 6, 7, 33, 45, 61, 67, 130, 251, 510, 1021])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_rows_that_end_with_a_part_of_a_four(E, dtype):
+    """The same bits as with experts that are out up to the next multiple of four, wherever the rows lie, and nothing beside the rows is written."""
+    rng = np.random.default_rng(E)
+    dtype, T, k, W = TYPES[dtype], 300, 2, -(-E // 4) * 4
+    padded = torch.full((T, W), -float("inf"), dtype=dtype, device=DEV)
+    padded[:, :E], _ = _logits(rng, T, E, dtype, out=0.1)
+    it, _ = _picks(rng, T, E, k, strange=False)             # an index of E is no expert of one side, and of the other one that is out
+    teacher = _logits(rng, T, 4, torch.float32)[0], torch.full((T,), 3.0, device=DEV)
+    ti = _dev(rng.integers(0, E, size=(T, 4)).astype(np.int32))
+    g = _dev(rng.normal(size=(T, k)).astype(np.float32))
+
+    def everything(x, place):
+        outs = [v for m in (0, 1, min(E, 8), min(E, 16)) for v in rs.route_logprobs(x, it, alternatives=m) if v is not None]
+        counts, tokens, sums, loss = rs.route_balance(x, it)
+        outs += [counts[:, :E], tokens, sums[:, :E], rs.route_distill(x, ti, teacher[0], teacher[1])]
+        grads = []
+        for add in (False, True):
+            grads.append(rs.route_logprobs_backward(x, it, g, g[:, 0].contiguous(), g[:, 1].contiguous(), accumulate=add, out=place).clone())
+            grads.append(rs.route_balance_backward(x, k, counts, tokens, torch.ones(1, device=DEV), accumulate=add, out=place).clone())
+            grads.append(rs.route_distill_backward(x, ti, teacher[0], g[:, 0].contiguous(), teacher[1], accumulate=add, out=place).clone())
+        return outs, [v[:, :E] for v in grads]
+
+    want, want_grads = everything(padded, torch.empty_like(padded))
+    for shift in range(4):
+        for ld in (E, E + 1, W):
+            room = torch.full((T * ld + 8,), 5.0, dtype=dtype, device=DEV)
+            x = room[shift:shift + T * ld].view(T, ld)[:, :E]
+            x.copy_(padded[:, :E])
+            to = torch.full((T * ld + 8,), 7.0, dtype=dtype, device=DEV)
+            place = to[3 - shift:3 - shift + T * ld].view(T, ld)[:, :E]
+            got, grads = everything(x, place)
+            what = f"{shift} values off, {ld} apart"
+            if shift == 0 and ld == E:                      # a balance loss counts the experts, and its gradient is in these
+                for i in (1, 4, 5):
+                    want_grads[i] = grads[i]
+            for a, b in zip(want, got):
+                assert torch.equal(a, b), what
+            for a, b in zip(want_grads, grads):
+                assert torch.equal(a, b), what
+            place.fill_(7.0)
+            assert bool((to == 7.0).all()), what
