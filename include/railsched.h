@@ -313,7 +313,7 @@ int railsched_port_round_robin(const int64_t *chunk_off, const uint8_t *rail, in
  *             sum rounded to `dtype`; rows that do not count are left as they are).
  *   An index outside [0,E) is ignored.
  * Limits: E <= 1024, k, m and K <= E, m and K <= 64, rows < 2^31, ld and ld_d <= 2^31, groups <= 2^23.  rows may be 0 (nothing is written but the groups' outputs).
- * Errors: NULL_PTR, INVALID_ARG (sizes, ld < E, unknown dtype, temperature out of range, accumulate not 0 or 1,
+ * Errors: NULL_PTR, INVALID_ARG (sizes, ld < E, unknown dtype, temperature out of range, accumulate not 0 or 1 (or 2 where it says so),
  * d_logits == logits), UNSUPPORTED (limits), WORKSPACE.
  * ------------------------------------------------------------------------------------------- */
 typedef enum railsched_dtype { RAILSCHED_F32 = 0, RAILSCHED_BF16 = 1, RAILSCHED_F16 = 2 } railsched_dtype;
@@ -359,7 +359,7 @@ int railsched_route_balance(const void *logits, int32_t dtype, int64_t rows, int
 
 /* Its gradient through the probabilities (the counts are constants): with a_e = d_loss[g] coef E c_e / (k n^2),
  * d_logits[e] = p_e (a_e - sum_f a_f p_f).  counts and tokens are inputs: a caller that adds them up over ranks first trains on
- * the balance of all of them.  Rows of no group are left as they are.
+ * the balance of all of them.  Rows of no group are left as they are, but set to 0 with accumulate = 2, which is 0 otherwise.
  *   counts [groups][E] int64, tokens [groups] int64, d_loss [groups] fp32       (in) */
 int railsched_route_balance_backward(const void *logits, int32_t dtype, int64_t rows, int32_t E, int64_t ld, const uint8_t *row_mask,
                                      int32_t k, const int64_t *group_off, int32_t groups, float coef, const int64_t *counts,

@@ -290,7 +290,7 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
                                                                      const uint8_t *__restrict__ row_mask, int k, Groups groups,
                                                                      int slice_rows, float coef, const int64_t *__restrict__ counts,
                                                                      const int64_t *__restrict__ tokens, const float *__restrict__ d_loss,
-                                                                     int add, T *__restrict__ d_logits, int64_t ld_d)
+                                                                     int add, int clear, T *__restrict__ d_logits, int64_t ld_d)
 {
     constexpr int ROWS_PER_BLOCK = 256 / LANES;
     __shared__ double part[4], total;
@@ -299,6 +299,14 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
     const int64_t r0 = first_row(slice_rows);
     if (r0 >= groups.rows) return;
     const int64_t r1 = r0 + slice_rows < groups.rows ? r0 + slice_rows : groups.rows;
+    if (clear) {                                         // the rows before the first group and behind the last one
+        const int64_t begin = groups.begin(0), end = groups.begin(groups.n);
+        float none[VPL];
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) none[j] = 0.0f;
+        for (int64_t w = r0 + slot; w < r1; w += ROWS_PER_BLOCK)
+            if (w < begin || w >= end) row_store<T, LANES, VPL, VEC, PARTS>(d_logits + w * ld_d, E, q, false, none);
+    }
     for (GroupWalk walk(groups, groups.holding(r0)); walk.g < groups.n; walk.next(groups)) {
         const int g = walk.g;
         const int64_t gb = walk.begin(), ge = walk.end();
@@ -487,7 +495,7 @@ extern "C" int railsched_route_balance_backward(const void *logits, int32_t dtyp
 {
     using namespace rs;
     if (int rc = check_router(logits, dtype, rows, E, ld, 1.0f)) return rc;
-    if (int rc = check_gradient(logits, d_logits, rows, E, ld_d, accumulate)) return rc;
+    if (int rc = check_gradient(logits, d_logits, rows, E, ld_d, accumulate == 2 ? 0 : accumulate)) return rc;
     if (k < 1 || k > E) return RAILSCHED_ERR_INVALID_ARG;
     if (int rc = check_groups(rows, group_off, groups)) return rc;
     if (groups == 0 || rows == 0) return RAILSCHED_OK;
@@ -501,8 +509,8 @@ extern "C" int railsched_route_balance_backward(const void *logits, int32_t dtyp
             const int slice_rows = gradient_slice_rows(rows, (int)sizeof(T) * E, 256 / S::LANES);
             auto go = [&](auto parts) {
                 hipLaunchKernelGGL((route_balance_backward_kernel<T, S::LANES, S::VPL, S::VEC, decltype(parts)::value>), row_grid(rows, slice_rows), dim3(256), 0, st,
-                                   static_cast<const T *>(logits), E, ld, row_mask, k, gr, slice_rows, coef, counts, tokens, d_loss, accumulate,
-                                   static_cast<T *>(d_logits), ld_d);
+                                   static_cast<const T *>(logits), E, ld, row_mask, k, gr, slice_rows, coef, counts, tokens, d_loss, accumulate == 1,
+                                   accumulate == 2 && group_off, static_cast<T *>(d_logits), ld_d);
                 return launch_status();
             };
             return S::VEC && E % 4 != 0 ? go(std::integral_constant<bool, S::VEC>()) : go(std::false_type());

@@ -792,3 +792,31 @@ def test_rows_that_end_with_a_part_of_a_four(E, dtype):
                 assert torch.equal(a, b), what
             place.fill_(7.0)
             assert bool((to == 7.0).all()), what
+
+
+@pytest.mark.parametrize("cuts", [[0, 0], [100, 100, 100], [7, 400, 993], [0, 500, 1000], [1000, 1000], [640, 1000], [0, 3]])
+@pytest.mark.parametrize("E,dtype", [(8, "fp32"), (61, "bf16"), (256, "fp32")])
+def test_rows_of_no_group_have_no_gradient(cuts, E, dtype):
+    """Without `out` the rows before the first group and behind the last one are 0, whatever they hold; the others are what they are with it."""
+    rng = np.random.default_rng(E)
+    T, k = 1000, 2
+    xt, _ = _logits(rng, T, E, TYPES[dtype])
+    it, _ = _picks(rng, T, E, k)
+    xt[:cuts[0]] = float("nan")
+    xt[cuts[-1]:] = float("inf")
+    off = torch.tensor(cuts, device=DEV)
+    counts, tokens, _, loss = rs.route_balance(xt, it, group_off=off)
+    want = torch.zeros_like(xt)
+    rs.route_balance_backward(xt, k, counts, tokens, torch.ones_like(loss), group_off=off, out=want)
+    for _ in range(2):
+        dirty = torch.full_like(xt, float("nan"))           # what the allocator hands out next
+        del dirty
+        got = rs.route_balance_backward(xt, k, counts, tokens, torch.ones_like(loss), group_off=off)
+        assert torch.equal(got, want)
+    assert not bool(want[:cuts[0]].any()) and not bool(want[cuts[-1]:].any()) and bool(want.isfinite().all())
+
+
+def test_no_group_at_all_has_no_gradient():
+    x = torch.randn((50, 8), device=DEV)
+    none = torch.zeros((0, 8), dtype=torch.int64, device=DEV), torch.zeros(0, dtype=torch.int64, device=DEV), torch.zeros(0, device=DEV)
+    assert not bool(rs.route_balance_backward(x, 2, *none, group_off=torch.zeros(1, dtype=torch.int64, device=DEV)).any())
