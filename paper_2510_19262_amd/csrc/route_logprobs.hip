@@ -206,9 +206,13 @@ __global__ __launch_bounds__(256) void route_logprobs_backward_kernel(const T *_
     const bool counts = at_row.live && soft.total != 0.0f;
     const float scale = inverse(soft.total), pull = sum - along;
     if (d_entropy) {
+        // p goes into the difference before d_entropy does: an expert that is out, or nearly, has p (y - mean) small however far y is, where d_entropy (y - mean) may overflow
         const float mean = row_dot<LANES, VPL>(y, e) * scale;
 #pragma unroll
-        for (int j = 0; j < VPL; ++j) dx[j] -= e[j] * scale * (pull + spread * (fmaxf(y[j], -1e30f) - mean));
+        for (int j = 0; j < VPL; ++j) {
+            const float p = e[j] * scale;
+            dx[j] -= p * pull + spread * (p * (fmaxf(y[j], -1e30f) - mean));
+        }
     } else {
 #pragma unroll
         for (int j = 0; j < VPL; ++j) dx[j] -= e[j] * scale * pull;
