@@ -359,7 +359,8 @@ int railsched_route_balance(const void *logits, int32_t dtype, int64_t rows, int
 
 /* Its gradient through the probabilities (the counts are constants): with a_e = d_loss[g] coef E c_e / (k n^2),
  * d_logits[e] = p_e (a_e - sum_f a_f p_f).  counts and tokens are inputs: a caller that adds them up over ranks first trains on
- * the balance of all of them.  Rows of no group are left as they are, but set to 0 with accumulate = 2, which is 0 otherwise.
+ * the balance of all of them.  Rows of no group are left as they are, but set to 0 with accumulate = 2, which is 0 otherwise
+ * (with groups = 0 and group_off given that is every row; counts, tokens and d_loss may be NULL then).
  *   counts [groups][E] int64, tokens [groups] int64, d_loss [groups] fp32       (in) */
 int railsched_route_balance_backward(const void *logits, int32_t dtype, int64_t rows, int32_t E, int64_t ld, const uint8_t *row_mask,
                                      int32_t k, const int64_t *group_off, int32_t groups, float coef, const int64_t *counts,

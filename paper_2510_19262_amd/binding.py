@@ -673,8 +673,6 @@ def route_balance_backward(logits: torch.Tensor, k: int, counts: torch.Tensor, t
     r = _Rows(logits)
     n, off = _groups(r, counts.shape[0], group_off)
     how = 2 if out is None and off is not None else int(accumulate)        # 2: rows of no group are set to 0
-    if how == 2 and n == 0 and not accumulate:
-        return torch.zeros((r.rows, r.E), dtype=r.dtype, device=r.device)
     out, to, ld_d = r.gradient(out, accumulate)
     r.call("railsched_route_balance_backward", *r.head, r.mask(row_mask), k, off, n, coef, r.arg(counts, torch.int64, (n, r.E), "counts"),
            r.arg(tokens, torch.int64, (n,), "tokens"), r.arg(d_loss, torch.float32, (n,), "d_loss"), how, to, ld_d)

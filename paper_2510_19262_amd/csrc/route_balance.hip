@@ -299,7 +299,7 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
     const int64_t r0 = first_row(slice_rows);
     if (r0 >= groups.rows) return;
     const int64_t r1 = r0 + slice_rows < groups.rows ? r0 + slice_rows : groups.rows;
-    if (clear) {                                         // the rows before the first group and behind the last one
+    if (clear) {                                         // the rows before the first group and behind the last one; all, where there is no group
         const int64_t begin = groups.begin(0), end = groups.begin(groups.n);
         float none[VPL];
 #pragma unroll
@@ -498,8 +498,9 @@ extern "C" int railsched_route_balance_backward(const void *logits, int32_t dtyp
     if (int rc = check_gradient(logits, d_logits, rows, E, ld_d, accumulate == 2 ? 0 : accumulate)) return rc;
     if (k < 1 || k > E) return RAILSCHED_ERR_INVALID_ARG;
     if (int rc = check_groups(rows, group_off, groups)) return rc;
-    if (groups == 0 || rows == 0) return RAILSCHED_OK;
-    if (!counts || !tokens || !d_loss) return RAILSCHED_ERR_NULL_PTR;
+    const bool clear = accumulate == 2 && group_off;
+    if (rows == 0 || (groups == 0 && !clear)) return RAILSCHED_OK;
+    if (groups > 0 && (!counts || !tokens || !d_loss)) return RAILSCHED_ERR_NULL_PTR;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const Groups gr = make_groups(rows, group_off, groups);
     return by_dtype(dtype, [&](auto t) {
@@ -510,7 +511,7 @@ extern "C" int railsched_route_balance_backward(const void *logits, int32_t dtyp
             auto go = [&](auto parts) {
                 hipLaunchKernelGGL((route_balance_backward_kernel<T, S::LANES, S::VPL, S::VEC, decltype(parts)::value>), row_grid(rows, slice_rows), dim3(256), 0, st,
                                    static_cast<const T *>(logits), E, ld, row_mask, k, gr, slice_rows, coef, counts, tokens, d_loss, accumulate == 1,
-                                   accumulate == 2 && group_off, static_cast<T *>(d_logits), ld_d);
+                                   clear, static_cast<T *>(d_logits), ld_d);
                 return launch_status();
             };
             return S::VEC && E % 4 != 0 ? go(std::integral_constant<bool, S::VEC>()) : go(std::false_type());

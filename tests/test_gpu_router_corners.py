@@ -39,3 +39,39 @@ def test_entropy_gradient_of_any_size_where_experts_are_out(E, size, dtype):
         out[:, 0] &= not with_logp                                  # a pick that is out has its slot's gradient
         assert not bool(got[out].any())
         _gradient_near(got, want, mag, x, 1.0, dtype, 1, 3 * _delta(x, 1.0), "gradient")
+
+
+@pytest.mark.parametrize("rows,E", [(1, 1), (5, 8), (300, 11), (70, 61), (4000, 64), (33, 1024)])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_gradient_without_a_group_through_the_c_entry(rows, E, dtype):
+    """accumulate = 2 sets every row to 0 where there is no group, whatever the rows, the mask and the memory hold; 0 and 1 leave them."""
+    from paper_2510_19262_amd import binding
+    code, dtype = binding.DTYPES[TYPES[dtype]], TYPES[dtype]
+    x = torch.full((rows, E), float("nan"), dtype=dtype, device=DEV)
+    mt = torch.zeros(rows, dtype=torch.uint8, device=DEV)
+    for first in (-3, 0, rows // 2, rows, 1 << 40):
+        off = torch.tensor([first], device=DEV)
+        for mask in (None, mt.data_ptr()):
+            for how in (2, 0, 1):
+                place = torch.full((rows + 1, E + 3), 7.0, dtype=dtype, device=DEV)
+                place[:rows, :E] = float("nan")
+                rc = rs.load().railsched_route_balance_backward(x.data_ptr(), code, rows, E, E, mask, 1, off.data_ptr(), 0, 1.0, None, None, None, how,
+                                                                place.data_ptr(), E + 3, torch.cuda.current_stream().cuda_stream)
+                assert rc == 0
+                d = place[:rows, :E]
+                assert bool((d == 0).all()) if how == 2 else bool(d.isnan().all())
+                assert bool((place[:, E:] == 7.0).all()) and bool((place[rows] == 7.0).all())
+
+
+def test_gradient_without_a_group_is_checked_as_any_other():
+    x = torch.randn((50, 8), device=DEV)
+    none = torch.zeros((0, 8), dtype=torch.int64, device=DEV), torch.zeros(0, dtype=torch.int64, device=DEV), torch.zeros(0, device=DEV)
+    off = torch.zeros(1, dtype=torch.int64, device=DEV)
+    dirty = torch.full_like(x, float("nan"))                # what the allocator hands out next
+    del dirty
+    assert torch.equal(rs.route_balance_backward(x, 2, *none, group_off=off), torch.zeros_like(x))
+    for k in (0, 9):
+        with pytest.raises(rs.RailschedError):
+            rs.route_balance_backward(x, k, *none, group_off=off)
+    with pytest.raises(ValueError):
+        rs.route_balance_backward(x, 2, none[0], none[1].int(), none[2], group_off=off)
