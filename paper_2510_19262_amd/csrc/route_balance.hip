@@ -72,7 +72,7 @@ struct Records {
     __device__ __forceinline__ float *at(int64_t r, int64_t group) const { return data + (r + (per ? group * per : group)) * words; }
 };
 
-constexpr int kMaxGroups = 1 << 23;                     // a workgroup each, within the work-items that a grid counts
+constexpr int kMaxGroups = 1 << 23;                     // a workgroup of 256 threads each: half the work-items that a grid counts
 constexpr int kTile = 32;                               // columns of a tile where a grid of them joins the records
 
 // v added up over the lanes that are a multiple of LANES away from this one, in all of them
@@ -471,7 +471,8 @@ extern "C" int railsched_route_balance(const void *logits, int32_t dtype, int64_
         });
         if (rc || cut.per == 1) return rc;
     }
-    // a workgroup for every tile of columns where a group has many records; otherwise one for the group, whose tile is all of them
+    // a workgroup for every tile of columns where a group has many records; otherwise one for the group, whose tile is all of them, or 256 columns in turn where workgroups
+    // of 1024 threads would be 2^32 work-items, which is one more than a launch can have
     const int64_t slice_rows = cut.slice_rows > 0 ? cut.slice_rows : 1;
     auto join = [&](auto threads, auto tile, unsigned tiles) {
         hipLaunchKernelGGL((route_balance_join_kernel<decltype(threads)::value, decltype(tile)::value>), dim3((unsigned)groups, tiles), dim3(decltype(threads)::value),
@@ -484,7 +485,7 @@ extern "C" int railsched_route_balance(const void *logits, int32_t dtype, int64_
     if (cut.records / groups > 16) return join(large, std::integral_constant<int, kTile>(), (unsigned)balance_tiles(E));
     if (E <= kTile) return join(small, std::integral_constant<int, kTile>(), 1);
     if (E <= 64) return join(small, narrow, 1);
-    if (E <= 256) return join(small, small, 1);
+    if (E <= 256 || groups >= 1 << 22) return join(small, small, 1);
     return join(large, large, 1);
 }
 

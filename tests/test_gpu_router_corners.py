@@ -75,3 +75,36 @@ def test_gradient_without_a_group_is_checked_as_any_other():
             rs.route_balance_backward(x, k, *none, group_off=off)
     with pytest.raises(ValueError):
         rs.route_balance_backward(x, 2, none[0], none[1].int(), none[2], group_off=off)
+
+
+@pytest.mark.parametrize("groups,E,rows", [((1 << 22) - 1, 257, 3000), (1 << 22, 257, 3000), (1 << 22, 700, 0), ((1 << 22) + 5, 513, 999), (1 << 23, 260, 5000), (1 << 23, 8, 5000)])
+def test_as_many_groups_as_there_may_be(groups, E, rows):
+    """Most of them empty; up to 2^23, whatever the number of experts."""
+    rng = np.random.default_rng(groups % 1000 + E)
+    xt, x = _logits(rng, rows, E, torch.float32)
+    k = 2
+    idx = rng.integers(0, E, size=(rows, k))
+    cuts = np.sort(rng.integers(0, rows + 1, size=groups + 1))
+    cuts[0], cuts[-1] = 0, rows
+    off = _dev(cuts)
+    counts, tokens, sums, loss = rs.route_balance(xt, _dev(idx.astype(np.int32)), group_off=off, coef=1.0)
+    n = np.diff(cuts)
+    assert torch.equal(tokens, _dev(n))
+    some = np.flatnonzero(n)
+    edges = [(int(cuts[g]), int(cuts[g + 1])) for g in some]
+    wc, wn, ws, wl = R.balance(x, idx, edges, 1.0)
+    at = _dev(some)
+    assert torch.equal(counts[at], _dev(wc)) and int(counts.sum()) == rows * k
+    most = max(int(n.max()), 1) if rows else 1
+    worst = (_delta(x, 1.0).max() if rows else 0.0) + most * U
+    _near(sums[at], ws, worst * ws + 2 * most * U, "prob_sum")
+    share = E / (k * np.maximum(wn, 1.0) ** 2) * wc.sum(axis=1)
+    _near(loss[at], wl, wl * (worst + 2 * U) + share * 2 * most * U, "loss")
+    empty = tokens == 0
+    assert not bool(loss[empty].any()) and int((sums.amax(1) > 0).sum()) == len(some) and bool((sums.amin(1) >= 0).all())
+    d = rs.route_balance_backward(xt, k, counts, tokens, torch.ones(groups, device=DEV), group_off=off)
+    want, size = R.balance_backward(x, k, edges, 1.0, wc, wn, np.ones(len(some)))
+    if rows:
+        _gradient_near(d, want, size, x, 1.0, torch.float32, 8, 3 * _delta(x, 1.0), "gradient")
+    del counts, sums, loss, tokens, d
+    torch.cuda.empty_cache()
