@@ -323,7 +323,8 @@ typedef enum railsched_dtype { RAILSCHED_F32 = 0, RAILSCHED_BF16 = 1, RAILSCHED_
  *   logp      [rows][k] fp32: z[topk_idx] - lse; exp(logp) is the gate weight of the pick; 0 where ignored      (out)
  *   lse       [rows] fp32                                                                                     (out, nullable)
  *   entropy   [rows] fp32: -sum p log p                                                                       (out, nullable)
- *   alt_idx   [rows][m] int32: the experts of the m largest logits in stage 1's order; -1 where fewer are left (out; NULL iff m == 0)
+ *   alt_idx   [rows][m] int32: the experts of the m largest logits in stage 1's order; -1 where fewer are left (out; NULL iff m == 0).
+ *             NaN is no number and never among them; +infinity is
  *   alt_logp  [rows][m] fp32: their z - lse; -infinity where alt_idx is -1 in a row that counts               (out; NULL iff m == 0)
  * The logits of a row are read once; the picks' logits are fetched from the cache. */
 int railsched_route_logprobs(const void *logits, int32_t dtype, int64_t rows, int32_t E, int64_t ld, float temperature,

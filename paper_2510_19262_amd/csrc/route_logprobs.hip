@@ -121,7 +121,8 @@ __global__ __launch_bounds__(256) void route_logprobs_kernel(const T *__restrict
             int own[L];
             unsigned bits, u[KM];
             lane_best<LANES, VPL, L, false>(v, E, q, own, bits);
-            const bool bad = row_best<LANES, VPL, L, KM>(own, bits, m, u);
+            // a NaN has a place among the keys, above or below all numbers, but none in the order: a row with one (its total is NaN) goes by rounds, as narrow rows do
+            const bool bad = row_best<LANES, VPL, L, KM>(own, bits, m, u) || soft.total != soft.total;
             if (__ballot(there && bad) == 0ull) {
 #pragma unroll
                 for (int r = 0; r < (KM + LANES - 1) / LANES; ++r) {     // alternatives q, q + LANES, ... of this lane

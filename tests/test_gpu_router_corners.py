@@ -108,3 +108,44 @@ def test_as_many_groups_as_there_may_be(groups, E, rows):
         _gradient_near(d, want, size, x, 1.0, torch.float32, 8, 3 * _delta(x, 1.0), "gradient")
     del counts, sums, loss, tokens, d
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("E", [8, 32, 36, 61, 64, 100, 128, 250, 256, 400, 512, 1000, 1024])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_alternatives_of_rows_with_nan(E, dtype):
+    """The numbers of such a row in their order, and no NaN, in every way of finding the largest and whatever rows are beside it."""
+    rng = np.random.default_rng(E)
+    T, inf, nan = 96, float("inf"), float("nan")
+    xt, x = _logits(rng, T, E, TYPES[dtype])
+    strange = np.arange(0, T, 5)                            # rows with NaN among rows without
+    for i, r in enumerate(strange):
+        at = rng.permutation(E)
+        if i % 4 == 0:
+            x[r, at[0]] = nan
+        elif i % 4 == 1:                                    # few numbers left, -NaN and +NaN
+            x[r] = -inf
+            x[r, at[:3]] = [1.0, -2.0, 1.0]
+            x[r, at[3:5]] = [nan, np.copysign(nan, -1.0)]
+        elif i % 4 == 2:
+            x[r, at[:2]] = [inf, nan]
+        else:
+            x[r] = nan
+    xt.copy_(torch.from_numpy(x).to(DEV))
+    ties = xt.clone()
+    for r in range(T):
+        if r not in strange:
+            ties[r] = 1.0                                   # the rows beside them: all ties
+    order = [[e for e in np.argsort(-np.where(np.isnan(row), -inf, row), kind="stable") if row[e] > -inf] for row in x]
+    for m in sorted({1, min(E, 4), min(E, 8), min(E, 9), min(E, 16), min(E, 20)}):
+        ai, al = rs.route_logprobs(xt, alternatives=m)[3:]
+        for r in strange:
+            want = (order[r] + [-1] * m)[:m]
+            assert ai[r].tolist() == want, f"row {r}, {m} alternatives"
+            assert all(np.isnan(v) if e >= 0 else v == -inf for e, v in zip(want, al[r].tolist()))
+            alone = rs.route_logprobs(xt[r:r + 1], alternatives=m)[3:]
+            assert torch.equal(alone[0][0], ai[r]) and torch.equal(alone[1][0].isnan(), al[r].isnan())
+        beside, _ = rs.route_logprobs(ties, alternatives=m)[3:]
+        assert torch.equal(beside[_dev(strange)], ai[_dev(strange)])
+        for r in range(T):                                  # and they do not reach the others
+            if r not in strange:
+                assert ai[r].tolist() == order[r][:m]
