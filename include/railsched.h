@@ -307,7 +307,7 @@ int railsched_port_round_robin(const int64_t *chunk_off, const uint8_t *rail, in
  *   row_mask  [rows] uint8, NULL = all rows count.  A row whose entry is 0 (padding) does not count, and neither does a
  *             row whose logits are all -infinity: whatever a masked row holds enters nothing, its picks are not counted, its
  *             floating outputs and its gradient are 0, its alternatives -1.
- *   temperature  tau, within 2^-60 .. 2^60: z = logits / tau, p = softmax(z) over the row, lse = log sum exp z.
+ *   temperature  tau, within 2^-60 .. 2^60 (distillation: 2^-8 .. 2^8): z = logits / tau, p = softmax(z) over the row, lse = log sum exp z.
  *   d_logits  the gradient, type `dtype`, row r at d_logits + r*ld_d, ld_d >= E; not the same memory as logits.  Places
  *             between the rows are left as they are.  accumulate = 0: overwritten; 1: added to what is there (each
  *             sum rounded to `dtype`; rows that do not count are left as they are).
@@ -377,6 +377,9 @@ int railsched_route_balance_backward(const void *logits, int32_t dtype, int64_t 
  *   loss[r] = tau^2 (sum_j q_j (log q_j - log p[t_idx[j]]) + q_r (log q_r - log p_r))
  * A row without entries has the loss 0 (also with t_lse).  +infinity where q_j > 0 meets an expert that is out.
  * An expert listed twice counts with the sum of its entries' terms.
+ * temperature is within 2^-8 .. 2^8: log p - log q, from which loss and gradient are formed, is off by a few 2^-24 of 1 + |logit - t_logit| / tau, while it is itself of
+ * order 1 / tau for a large tau.  A gradient is off by about 2^-11 of itself at most at either end where student and teacher differ by about 1; a t_lse counts as the number that it is in
+ * fp32 (with a list that leaves p no rest, half a step of t_lse changes the loss by tau^2 times that).
  *   t_idx [rows][K] int32, t_logit [rows][K] fp32, t_lse [rows] fp32 (nullable)  (in; alt_idx and alt_logp of railsched_route_logprobs
  *                                                                                will do, with t_lse = 0 at temperature 1)
  *   loss  [rows] fp32                                                            (out) */

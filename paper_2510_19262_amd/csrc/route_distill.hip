@@ -5,8 +5,8 @@
 // it where the list holds nearly everything).
 //
 // The loss is formed as  sum_j (q log(q/p) - q + p) + rest + (sum of q and p outside these terms):  every term is >= 0 and of second order where
-// p is near q, so a student near its teacher keeps its loss to fp32's relative accuracy, where sum q (log q - log p) would be a difference of
-// larger terms.  With d = log p - log q:  q log(q/p) - q + p = q (e^d - 1 - d).
+// p is near q, where sum q (log q - log p) would be a difference of larger terms.  With d = log p - log q:  q log(q/p) - q + p = q (e^d - 1 - d), so that an error of
+// d, a few 2^-24 of 1 + |logit - t_logit| / tau, costs |p - q| times that.
 //
 // The loss reads the logits and 8 bytes an entry: bound by the instructions where the logits are short (2^20 x 64 bf16 with 6 entries: 41 us for 0.19 GB, 390 vector
 // instructions for 16 rows), nearly by the reads where they are not (2^20 x 256 fp32: 176 us for 1.15 GB).  The gradient reads and writes every logit: 2^20 x 256 with 8 entries
@@ -244,9 +244,14 @@ __global__ __launch_bounds__(256) void route_distill_backward_kernel(const T *__
     if (at_row.there && (counts || !add)) row_store<T, LANES, VPL, VEC>(d_logits + (first + threadIdx.x / LANES) * ld_d, E, q0, add != 0, o.y);
 }
 
-static int check_distill(int64_t rows, int32_t E, const int32_t *t_idx, const float *t_logit, int32_t K)
+// The temperatures that fp32 carries.  d = log p - log q is off by a few 2^-24 times 1 + |logit - t_logit| / tau.  A large tau makes d itself small, of order 1 / tau, so that
+// the gradient loses tau 2^-24 of itself; a small one makes that error 2^-24 / tau of q.  Largest errors of 2000 rows of 64 experts, teacher within 0.5 of the student's
+// logits, as a share of a row's gradient: tau 32 7e-5, 256 4e-4, 2^14 2e-2, 10^6 more than all of it; as a share of tau d_loss: 2^-6 1e-5, 2^-8 5e-5, 10^-4 1e-3, 10^-6 0.06.
+constexpr float kLeastTau = 0x1p-8f, kMostTau = 0x1p8f;
+
+static int check_distill(int64_t rows, int32_t E, float temperature, const int32_t *t_idx, const float *t_logit, int32_t K)
 {
-    if (K < 1 || K > E) return RAILSCHED_ERR_INVALID_ARG;
+    if (K < 1 || K > E || !(temperature >= kLeastTau) || !(temperature <= kMostTau)) return RAILSCHED_ERR_INVALID_ARG;
     if (K > kMaxListed) return RAILSCHED_ERR_UNSUPPORTED;
     if (rows > 0 && (!t_idx || !t_logit)) return RAILSCHED_ERR_NULL_PTR;
     return RAILSCHED_OK;
@@ -260,7 +265,7 @@ extern "C" int railsched_route_distill(const void *logits, int32_t dtype, int64_
 {
     using namespace rs;
     if (int rc = check_router(logits, dtype, rows, E, ld, temperature)) return rc;
-    if (int rc = check_distill(rows, E, t_idx, t_logit, K)) return rc;
+    if (int rc = check_distill(rows, E, temperature, t_idx, t_logit, K)) return rc;
     if (rows == 0) return RAILSCHED_OK;
     if (!loss) return RAILSCHED_ERR_NULL_PTR;
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -285,7 +290,7 @@ extern "C" int railsched_route_distill_backward(const void *logits, int32_t dtyp
     using namespace rs;
     if (int rc = check_router(logits, dtype, rows, E, ld, temperature)) return rc;
     if (int rc = check_gradient(logits, d_logits, rows, E, ld_d, accumulate)) return rc;
-    if (int rc = check_distill(rows, E, t_idx, t_logit, K)) return rc;
+    if (int rc = check_distill(rows, E, temperature, t_idx, t_logit, K)) return rc;
     if (rows == 0) return RAILSCHED_OK;
     if (!d_loss) return RAILSCHED_ERR_NULL_PTR;
     hipStream_t st = static_cast<hipStream_t>(stream);

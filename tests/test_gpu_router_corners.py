@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from oracle import router as R
-from test_gpu_router import DEV, TYPES, U, _delta, _dev, _gradient_near, _logits, _near
+from test_gpu_router import DEV, TYPES, U, _delta, _dev, _gradient_near, _logits, _near, _teacher
 
 pytestmark = pytest.mark.gpu
 
@@ -149,3 +149,44 @@ def test_alternatives_of_rows_with_nan(E, dtype):
         for r in range(T):                                  # and they do not reach the others
             if r not in strange:
                 assert ai[r].tolist() == order[r][:m]
+
+
+@pytest.mark.parametrize("tau", [2.0 ** -8, 0.05, 32.0, 100.0, 256.0])
+@pytest.mark.parametrize("E,K,tail", [(64, 8, False), (64, 64, False), (64, 8, True), (61, 20, True), (256, 16, True), (8, 8, False), (1000, 30, True)])
+@pytest.mark.parametrize("near", [0.5, 2.0])
+def test_distillation_at_the_ends_of_its_temperatures(tau, E, K, tail, near):
+    """The bounds of test_gpu_router.test_distill hold up to the limits, where d = log p - log q is small (tau large) or its error is (tau small)."""
+    rng = np.random.default_rng(E + K)
+    T = 400
+    xt, x = _logits(rng, T, E, torch.float32, scale=1.0)
+    idx, logit, lse = _teacher(rng, x, K, tail, tau, near)
+    args, lt, l64 = (_dev(idx.astype(np.int32)), _dev(logit)), None if lse is None else _dev(lse), None if lse is None else lse.astype(float)
+    o = R.distill_terms(x, idx, logit.astype(float), l64, tau)
+    if tail:                                                # rows whose rest fp32 leaves out have a test of their own
+        fine = o["rest_p"] > 2.0 ** -100
+        if not fine.any():
+            pytest.skip("no row has a rest at this temperature")
+    else:
+        fine = np.ones(T, bool)
+    want = R.distill(x, idx, logit.astype(float), l64, tau)
+    loss = rs.route_distill(xt, *args, lt, temperature=tau)
+    p = np.take_along_axis(o["p"], idx, 1)
+    log_p = np.take_along_axis(o["z"], idx, 1) - o["lse"][:, None]
+    d = np.abs(log_p - (o["u"] - o["log_mass"][:, None]))
+    t = np.take_along_axis(x.max(axis=1, keepdims=True) - x, idx, 1) / tau
+    delta = 2 * _delta(x, tau, np.abs(logit).max(axis=1) / tau, *([np.abs(lse)] if tail else [])) + 2.5 * U * t.max(axis=1)
+    P = p.sum(axis=1)
+    large = np.where(d > 0.25, p + o["q"] * (1 + d), 0.0).sum(axis=1)
+    apart = np.abs(o["mass"] - P)
+    rest = np.where(o["rest_q"] > 0, apart / np.maximum(o["rest_p"], 1e-300) * (o["mass"] + P), o["rest_p"] + (o["mass"] if tail else 0.0))
+    # d's error in the second order too: delta^2, which is all there is where p is q
+    tol = tau * tau * (delta * (np.abs(p - o["q"]).sum(axis=1) + large + rest) + delta * delta) + np.abs(want) * 64 * U + 2.0 ** -100
+    _near(loss[_dev(fine)], want[fine], tol[fine], "loss")
+    g = rng.normal(size=T).astype(np.float32)
+    got = rs.route_distill_backward(xt, *args, _dev(g), lt, temperature=tau)
+    wd, size = R.distill_backward(x, idx, logit.astype(float), g.astype(float), l64, tau)
+    size = size + np.abs(tau * g)[:, None] * o["p"] * np.where(o["rest_q"] > 0, (o["mass"] + P) / np.maximum(o["rest_p"], 1e-300), 0.0)[:, None]
+    _gradient_near(got[_dev(fine)], wd[fine], size[fine], x[fine], tau, torch.float32, K, 2 * delta[fine], "gradient")
+    # and what the header says of either end: about 2^-11 of the gradient, or of tau d_loss, for differences of about 1; 2^-9 here, where they are 0.5 to several
+    off = np.abs(got.double().cpu().numpy() - wd).sum(axis=1)[fine]
+    assert (off <= 2.0 ** -9 * np.maximum(np.abs(wd).sum(axis=1), np.abs(tau * g))[fine]).all() if tau < 1 else (off <= 2.0 ** -9 * np.abs(wd).sum(axis=1)[fine]).all()
