@@ -511,6 +511,13 @@ def port_round_robin(chunk_off, rail, batch: int, topo: Topo, ports: int, capaci
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
+def _int32(v: int, name: str) -> int:
+    """v, refused where 32 bits do not hold it: the library would see another number."""
+    if not -(1 << 31) <= v < 1 << 31:
+        raise ValueError(f"{name} must fit 32 bits, got {v}")
+    return v
+
+
 class _Rows:
     """Checks of the operators on a router's logits: tensors on one device, launches on that device's current stream."""
     __slots__ = ("logits", "device", "dtype", "rows", "E", "head")
@@ -547,7 +554,7 @@ class _Rows:
             return 0
         if t.dim() != 2:
             raise ValueError(f"{name} must have two dimensions")
-        return t.shape[1]
+        return _int32(t.shape[1], f"the width of {name}")
 
     def arg(self, t: Optional[torch.Tensor], dtype, shape, name: str):
         """The address of a contiguous tensor of this type and shape on the logits' device; None for None."""
@@ -605,7 +612,7 @@ def route_logprobs(logits: torch.Tensor, topk_idx: Optional[torch.Tensor] = None
     experts: (logp or None, lse, entropy, alt_idx or None, alt_logp or None).  logits may be a view with a row stride.
     out: a tuple of the same five, preallocated (lse and entropy may be None there: not computed)."""
     r = _Rows(logits)
-    k, m = r.width(topk_idx, "topk_idx"), alternatives
+    k, m = r.width(topk_idx, "topk_idx"), _int32(alternatives, "alternatives")
     if out is None:
         out = (r.new((r.rows, k)) if k else None, r.new(r.rows), r.new(r.rows), r.new((r.rows, m), torch.int32) if m > 0 else None,
                r.new((r.rows, m)) if m > 0 else None)
@@ -638,7 +645,7 @@ def route_balance_workspace_bytes(rows: int, groups: int, E: int) -> int:
 
 def _groups(r: _Rows, groups: int, group_off: Optional[torch.Tensor]):
     if group_off is None:
-        return groups, None
+        return _int32(groups, "groups"), None
     if group_off.dim() != 1 or group_off.shape[0] < 1:
         raise ValueError("group_off must hold groups + 1 offsets")
     return group_off.shape[0] - 1, r.arg(group_off, torch.int64, group_off.shape, "group_off")
@@ -674,7 +681,7 @@ def route_balance_backward(logits: torch.Tensor, k: int, counts: torch.Tensor, t
     n, off = _groups(r, counts.shape[0], group_off)
     how = 2 if out is None and off is not None else int(accumulate)        # 2: rows of no group are set to 0
     out, to, ld_d = r.gradient(out, accumulate)
-    r.call("railsched_route_balance_backward", *r.head, r.mask(row_mask), k, off, n, coef, r.arg(counts, torch.int64, (n, r.E), "counts"),
+    r.call("railsched_route_balance_backward", *r.head, r.mask(row_mask), _int32(k, "k"), off, n, coef, r.arg(counts, torch.int64, (n, r.E), "counts"),
            r.arg(tokens, torch.int64, (n,), "tokens"), r.arg(d_loss, torch.float32, (n,), "d_loss"), how, to, ld_d)
     return out
 

@@ -190,3 +190,14 @@ def test_distillation_at_the_ends_of_its_temperatures(tau, E, K, tail, near):
     # and what the header says of either end: about 2^-11 of the gradient, or of tau d_loss, for differences of about 1; 2^-9 here, where they are 0.5 to several
     off = np.abs(got.double().cpu().numpy() - wd).sum(axis=1)[fine]
     assert (off <= 2.0 ** -9 * np.maximum(np.abs(wd).sum(axis=1), np.abs(tau * g))[fine]).all() if tau < 1 else (off <= 2.0 ** -9 * np.abs(wd).sum(axis=1)[fine]).all()
+
+
+@pytest.mark.parametrize("by", [1 << 32, -(1 << 32), 1 << 40])
+def test_numbers_that_32_bits_do_not_hold(by):
+    """They are refused, not cut to their low bits."""
+    x, it = torch.randn((4, 8), device=DEV), torch.zeros((4, 2), dtype=torch.int32, device=DEV)
+    counts, tokens, _, loss = rs.route_balance(x, it)
+    for call in (lambda: rs.route_balance_backward(x, 2 + by, counts, tokens, loss), lambda: rs.route_logprobs(x, it, alternatives=2 + by),
+                 lambda: rs.route_balance(x, it, groups=1 + by)):
+        with pytest.raises(ValueError):
+            call()
