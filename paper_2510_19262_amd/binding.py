@@ -508,6 +508,8 @@ def port_round_robin(chunk_off, rail, batch: int, topo: Topo, ports: int, capaci
 
 
 # ---------------------------------------------------------------------------------- a router in training
+# No part of torch's autograd: outputs are detached, also of logits that require a gradient.  The _backward calls give the logits' gradient, which goes on by
+# logits.backward(gradient).
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
@@ -610,7 +612,8 @@ def route_logprobs(logits: torch.Tensor, topk_idx: Optional[torch.Tensor] = None
                    row_mask: Optional[torch.Tensor] = None, out=None):
     """Log probabilities of the experts topk_idx [rows][k], log-sum-exp and entropy of every row, and its `alternatives` most likely
     experts: (logp or None, lse, entropy, alt_idx or None, alt_logp or None).  logits may be a view with a row stride.
-    out: a tuple of the same five, preallocated (lse and entropy may be None there: not computed)."""
+    out: a tuple of the same five, preallocated (lse and entropy may be None there: not computed).
+    The outputs are detached from autograd: route_logprobs_backward gives the logits' gradient."""
     r = _Rows(logits)
     k, m = r.width(topk_idx, "topk_idx"), _int32(alternatives, "alternatives")
     if out is None:
@@ -654,7 +657,8 @@ def _groups(r: _Rows, groups: int, group_off: Optional[torch.Tensor]):
 def route_balance(logits: torch.Tensor, topk_idx: torch.Tensor, groups: int = 1, group_off: Optional[torch.Tensor] = None, coef: float = 1.0,
                   row_mask: Optional[torch.Tensor] = None, out=None, ws: Optional[torch.Tensor] = None):
     """Balance loss of groups of rows: (counts [groups][E] int64, tokens [groups] int64, prob_sum [groups][E], loss [groups]).
-    The groups are `groups` equal parts of the rows, or with group_off (int64 offsets) the rows between neighbouring offsets."""
+    The groups are `groups` equal parts of the rows, or with group_off (int64 offsets) the rows between neighbouring offsets.
+    The outputs are detached from autograd: route_balance_backward gives the logits' gradient."""
     r = _Rows(logits)
     n, off = _groups(r, groups, group_off)
     k = r.width(topk_idx, "topk_idx")
@@ -688,7 +692,8 @@ def route_balance_backward(logits: torch.Tensor, k: int, counts: torch.Tensor, t
 
 def route_distill(logits: torch.Tensor, teacher_idx: torch.Tensor, teacher_logits: torch.Tensor, teacher_lse: Optional[torch.Tensor] = None,
                   temperature: float = 1.0, row_mask: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """Divergence of every row's distribution from the teacher's list [rows][K] (and, with teacher_lse, the rest of the teacher's mass)."""
+    """Divergence of every row's distribution from the teacher's list [rows][K] (and, with teacher_lse, the rest of the teacher's mass).
+    temperature: 2^-8 to 2^8.  The outputs are detached from autograd: route_distill_backward gives the logits' gradient."""
     r = _Rows(logits)
     K = r.width(teacher_idx, "teacher_idx")
     if out is None:

@@ -201,3 +201,34 @@ def test_numbers_that_32_bits_do_not_hold(by):
                  lambda: rs.route_balance(x, it, groups=1 + by)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_logits_of_a_gate_that_autograd_trains():
+    """What comes back is detached; the summed gradient goes on from the logits to the gate's weights."""
+    rng = np.random.default_rng(21)
+    T, H, E, k = 500, 16, 24, 4
+    tokens, weight = rng.normal(size=(T, H)).astype(np.float32), rng.normal(size=(E, H)).astype(np.float32) * np.float32(0.25)
+    w = _dev(weight).requires_grad_()
+    logits = _dev(tokens) @ w.t()
+    x = logits.detach().double().cpu().numpy()
+    it = rs.route_topk(logits.detach(), k)
+    idx = it.cpu().numpy()
+    logp, lse, entropy, ai, al = rs.route_logprobs(logits, it, alternatives=k)
+    counts, tokens_, sums, loss = rs.route_balance(logits, it, coef=0.1)
+    kl = rs.route_distill(logits, ai, al + 0.5)
+    assert not any(v.requires_grad for v in (logp, lse, entropy, al, sums, loss, kl))
+    g, gz = rng.normal(size=(T, k)).astype(np.float32), rng.normal(size=T).astype(np.float32)
+    grad = rs.route_logprobs_backward(logits, it, _dev(g), _dev(gz))
+    rs.route_balance_backward(logits, k, counts, tokens_, torch.ones_like(loss), coef=0.1, accumulate=True, out=grad)
+    rs.route_distill_backward(logits, ai, al + 0.5, torch.ones_like(kl), accumulate=True, out=grad)
+    assert not grad.requires_grad
+    logits.backward(grad)
+    a, sa = R.logprobs_backward(x, idx, g.astype(float), gz.astype(float), np.zeros(T))
+    c = R.balance(x, idx, [(0, T)], 0.1)
+    b, sb = R.balance_backward(x, k, [(0, T)], 0.1, c[0], c[1], np.ones(1))
+    d, sd = R.distill_backward(x, ai.cpu().numpy(), (al + 0.5).double().cpu().numpy(), np.ones(T))
+    want = (a + b + d).T @ tokens.astype(float)
+    # the gradient's error, 4 delta of its terms' magnitudes with t up to 2 Z, through the product, which adds T terms in fp32
+    size = (sa + sb + sd)
+    off = (size * (4 * _delta(x, 1.0)[:, None] + (5 * np.abs(x).max() + 8) * U)).T @ np.abs(tokens) + T * U * (np.abs(a + b + d).T @ np.abs(tokens))
+    _near(w.grad, want, off, "gradient of the gate")
