@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from oracle import router as R
-from test_gpu_router import DEV, TYPES, U, _delta, _dev, _gradient_near, _logits, _near, _teacher
+from test_gpu_router import DEV, TYPES, U, _delta, _dev, _gradient_near, _logits, _near, _picks, _teacher
 
 pytestmark = pytest.mark.gpu
 
@@ -232,3 +232,71 @@ def test_logits_of_a_gate_that_autograd_trains():
     size = (sa + sb + sd)
     off = (size * (4 * _delta(x, 1.0)[:, None] + (5 * np.abs(x).max() + 8) * U)).T @ np.abs(tokens) + T * U * (np.abs(a + b + d).T @ np.abs(tokens))
     _near(w.grad, want, off, "gradient of the gate")
+
+
+def _cuts(rng, T, groups, ragged):
+    if not ragged:
+        return np.arange(groups + 1) * (T // groups)
+    return np.sort(rng.integers(0, T + 1, size=groups + 1))
+
+
+SUMS = [  # rows, experts, groups, ragged: one record a group and many, one tile of columns and several, workgroups of 256 and 512 threads
+    (400_000, 2, 2, True), (400_000, 7, 2, True), (400_000, 7, 1500, True), (262_144, 8, 4, False), (262_144, 8, 1, False), (4096 * 37, 8, 4096, False),
+    (137_000, 61, 150, True), (137_500, 61, 1, False), (100_000, 100, 20, True), (60_000, 256, 3, True), (65_536, 256, 1, False), (27_900, 300, 150, True),
+    (9_000, 891, 7, True), (8_192, 1024, 2, False), (1_000, 1024, 40, True)]
+
+
+@pytest.mark.parametrize("T,E,groups,ragged", SUMS)
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_no_row_is_lost_in_the_sums(T, E, groups, ragged, dtype):
+    """Rows with one expert left have p = 1 there, and whole numbers below 2^24 add up exactly in any order: prob_sum is the number of rows."""
+    rng = np.random.default_rng(T + E)
+    cuts = _cuts(rng, T, groups, ragged)
+    left = rng.integers(0, E, size=T)
+    counted = rng.random(T) >= 0.1
+    x = torch.full((T, E), -float("inf"), dtype=TYPES[dtype], device=DEV)
+    x[torch.arange(T, device=DEV), _dev(left)] = _dev(rng.normal(size=T) * 3).to(TYPES[dtype])
+    x[_dev(~counted)] = float("nan")
+    picks = _dev(((left + 1) % E).astype(np.int32)).view(T, 1)
+    args = dict(group_off=_dev(cuts)) if ragged else dict(groups=groups)
+    counts, tokens, sums, loss = rs.route_balance(x, picks, row_mask=_dev(counted.astype(np.uint8)), **args)
+    group = np.searchsorted(cuts, np.arange(T), side="right") - 1
+    use = counted & (group >= 0) & (group < groups)
+    want = np.bincount(group[use] * E + left[use], minlength=groups * E).reshape(groups, E)
+    np.testing.assert_array_equal(sums.double().cpu().numpy(), want.astype(float))
+    np.testing.assert_array_equal(tokens.cpu().numpy(), want.sum(axis=1))
+    np.testing.assert_array_equal(counts.cpu().numpy(), np.roll(want, 1, axis=1))
+    n = np.maximum(want.sum(axis=1), 1).astype(float)
+    exact = E / (n * n) * (np.roll(want, 1, axis=1) * want).sum(axis=1)             # formed in fp64, rounded once
+    _near(loss, exact, exact * 2 * U, "loss")
+
+
+def test_sums_beyond_2_24():
+    """Where fp32 no longer holds every whole number the parts are added up in more bits, and the sum is rounded once."""
+    T = (1 << 25) + 1001
+    x = torch.full((T, 2), -float("inf"), dtype=torch.bfloat16, device=DEV)
+    left = torch.zeros(T, dtype=torch.int64, device=DEV)
+    left[::3] = 1
+    x.scatter_(1, left.view(T, 1), 0.5)
+    counts, tokens, sums, loss = rs.route_balance(x, left.to(torch.int32).view(T, 1))
+    want = torch.bincount(left, minlength=2)
+    assert torch.equal(counts[0], want) and int(tokens) == T and torch.equal(sums[0], want.double().float())
+    exact = 2.0 / float(T) ** 2 * float((want.double() ** 2).sum())
+    assert abs(float(loss) - exact) <= 2 * U * exact
+
+
+@pytest.mark.parametrize("T,E,groups,ragged", SUMS)
+def test_sums_by_the_length_of_their_chains(T, E, groups, ragged):
+    """fp32 additions are the rounds of a workgroup only: at least 512 workgroups of at least 4 rows share all rows (or one has a group of at most 16384 logits), then 6 steps over lanes and 7 over
+    wavefronts; the parts are added in fp64."""
+    rng = np.random.default_rng(T + E + 1)
+    cuts = _cuts(rng, T, groups, ragged)
+    xt, x = _logits(rng, T, E, torch.float32)
+    it, idx = _picks(rng, T, E, 2)
+    args = dict(group_off=_dev(cuts)) if ragged else dict(groups=groups)
+    counts, tokens, sums, loss = rs.route_balance(xt, it, **args)
+    wc, wn, ws, wl = R.balance(x, idx, list(zip(cuts[:-1], cuts[1:])), 1.0)
+    chain = max(-(-T // 2048), 0 if ragged else -(-min(T // groups, 16384 // E) // 4)) + 16
+    worst = _delta(x, 1.0).max() + (2.5 / np.e + chain) * U
+    # p's own error has 2.5 |t| u of itself: p |t| is at most 1/e of the row's, whose share of ws is not known: as many rows as there are
+    _near(sums, ws, worst * ws + 2.5 / np.e * wn[:, None] * U, "prob_sum")
