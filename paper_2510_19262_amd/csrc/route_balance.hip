@@ -6,7 +6,7 @@
 // are cut into slices, a workgroup each, whose parts are of one group or several; slices and groups are both in row order, so the part of group g in slice s can take
 // the record s + g: no two parts share it.
 //
-// Bound by the reads of logits and picks (2^25 x 8 with 2 picks: 1.34 GB in 210 us, 6.4 TB/s; one group of 2^20 x 256: 181 us), where the rows are few by a chain of dependent
+// Bound by the reads of logits and picks (2^25 x 8 with 2 picks: 1.34 GB in 209 us, 6.4 TB/s; one group of 2^20 x 256: 187 us), where the rows are few by a chain of dependent
 // reads (offsets, rows, records: 13 and 6 us for 300 sequences of 65537 x 61).  The gradient reads and writes every logit: 2^20 x 256 in 341 us, 6.3 TB/s.
 #include "router_core.hpp"
 
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(THREADS) void route_balance_join_kernel(Records rec
 
 // d_logits[e] = p_e (a_e - sum_f a_f p_f), a_e = d_loss coef E c_e / (k n^2).  The gradient does not change with a constant added to a: the mean
 // count is taken off first (fp64), so that nothing is lost where the counts are nearly equal.
-// PARTS costs this loop over rows 3% where there are none (2^20 x 256: 342 us, 357).
+// PARTS costs this loop over rows 4% where there are none (2^20 x 256: 342 us, 357): 60 scalar registers are spilled with it and 16 values to a lane, 2 without.
 template <typename T, int LANES, int VPL, bool VEC, bool PARTS>
 __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__restrict__ logits, int E, int64_t ld,
                                                                      const uint8_t *__restrict__ row_mask, int k, Groups groups,
@@ -357,10 +357,13 @@ __global__ __launch_bounds__(256) void route_balance_backward_kernel(const T *__
     }
 }
 
-// How the rows are shared out, in whole rounds of the rows that a workgroup has in hand.  At most as many workgroups as are resident at a time, as one more is another round for
+// How the rows are shared out, in whole rounds of the rows that a workgroup has in hand.  About as many workgroups as are resident at a time, as many more are another round for
 // all: of 256 threads where the groups are short, 8 on a CU with 4 values to a lane, 6 with 8, 5 with 16; of 512 threads, 3 or 2, where a group would have more than 8 records
-// of the smaller ones, so that its records stay few (289392 x 128 in 24 groups: 35 us with 504 workgroups, 44 with 528 of 1024 threads; 2^20 x 64 in 200 ragged
-// groups: 59 and 65; 200000 x 1000 in 150: 141, 155 of 256 threads).  Equal groups of at most 16384 logits have a workgroup of 256 threads each: one launch.
+// of the smaller ones, so that its records stay few (289392 x 128 in 24 groups: 34 us with 504 workgroups, 44 with 528 of 1024 threads; 2^20 x 64 in 200 ragged
+// groups: 54 and 65; 200000 x 1000 in 150: 141, 155 of 256 threads).  The registers hold one wavefront less in two places: ragged groups of rows read in fours, 4 values to a lane, have 7
+// workgroups on a CU, so that 256 and more of them leave a second round of an eighth; and ragged groups of 16 values to a lane spill 6 to 13 scalar registers.
+// Equal groups have whole workgroups, as many as fit or one each: with one each they are anything up to what is resident, or more (4096 x 256 a group: 512 groups
+// 319 us, 700 459, 1280 840, all 6.4 to 6.7 TB/s, but 1300 943, 5.8).  Equal groups of at most 16384 logits have a workgroup of 256 threads each: one launch.
 struct Cut {
     int threads, per;       // per: workgroups to a group; 0: slices
     int64_t slice_rows, blocks, records;
@@ -386,8 +389,8 @@ static Cut balance_cut(int64_t rows, int32_t groups, int E, bool equal)
     }
 }
 // Rows of a workgroup of the gradient: 16 KiB of logits, 32 KiB of rows of more than 256 bytes; whole rounds of the rows in hand; fewer where the GPU would not be full.  Much
-// more is slower by up to a third (2^20 x 256: 344 us with 32 KiB, 417 with 512; 2^21 x 64: 179 with 16, 235 with 256), less pays for the weights too often (2^23 x 8: 839 us
-// with 0.5 KiB, 92 with 16).
+// more is slower by up to a third (2^20 x 256: 340 us with 32 KiB, 417 with 512; 2^21 x 64: 178 with 16, 235 with 256), less pays for the weights too often (2^23 x 8: 135 us
+// with 4 KiB, which one round takes, 90 with 16; 2^20 x 256: 352 with 4).
 static int gradient_slice_rows(int64_t rows, int row_bytes, int in_hand)
 {
     int64_t r = (row_bytes <= 256 ? 16384 : 32768) / row_bytes;

@@ -9,19 +9,22 @@
 // d, a few 2^-24 of 1 + |logit - t_logit| / tau, costs |p - q| times that.
 //
 // The loss reads the logits and 8 bytes an entry: bound by the instructions where the logits are short (2^20 x 64 bf16 with 6 entries: 41 us for 0.19 GB, 390 vector
-// instructions for 16 rows), nearly by the reads where they are not (2^20 x 256 fp32: 176 us for 1.15 GB).  The gradient reads and writes every logit: 2^20 x 256 with 8 entries
-// and the tail 366 us, 6.1 TB/s.
+// instructions for 16 rows), nearly by the reads where they are not (2^20 x 256 fp32: 179 us for 1.15 GB).  Lists of more than two entries a lane take
+// registers: with 16 entries a lane 86 scalar ones are spilled and 4 wavefronts a SIMD are left of 8 (800393 x 64 fp16 with 32 entries: 138 us for 0.31 GB).  The gradient reads and writes every logit: 2^20 x 256 with 8 entries
+// and the tail 369 us, 6.0 TB/s.
 #include "router_core.hpp"
 
 namespace rs {
 
-// e^a for a few values, a <= 0 or near it: the product with log2 e is carried on to a second float, as its rounding alone is 2^-24 |a| of the result
+// e^a for a few values, a <= 0 or near it: the product with log2 e is carried on to a second float, as its rounding alone is 2^-24 |a| of the result.  low is what fl(a fl(log2 e)) leaves,
+// and a times what log2 e has behind its fp32 value
 __device__ __forceinline__ float exp_of(float a)
 {
     const float y = a * kLog2e, low = fmaf(a, 0x1.4ae0c0p-26f, fmaf(a, kLog2e, -y));
     return pow2(y) * (fabsf(low) < 1.0f ? fmaf(low, kLn2, 1.0f) : 1.0f);      // NaN where a is infinite
 }
-// a - log v of a normal v = m 2^k: k log 2 goes off in two parts, the first of them without rounding, as its sum with log m would be rounded at k
+// a - log v of a normal v = m 2^k: k log 2 goes off in two parts, the first of them without rounding, as its sum with log m would be rounded at k.  The first part is log 2 to nine bits, whose
+// product with an exponent of at most eight is exact, the second the rest of log 2 (the splitting of Cody and Waite, Software Manual for the Elementary Functions, 1980)
 __device__ __forceinline__ float less_log(float a, float v)
 {
     const float k = (float)__builtin_amdgcn_frexp_expf(v), m = __builtin_amdgcn_frexp_mantf(v);

@@ -3,8 +3,8 @@
 // One pass over a row, in powers of two: the largest logit, then total = sum 2^y and dot = sum 2^y y from the values in registers (y <= 0: relative to the
 // largest).  lse = largest / tau + ln 2 log2 total, entropy = ln 2 (log2 total - dot / total) (no cancellation: both terms are >= 0), and the picks' logits
 // are read again, from the cache.  It has to read the logits and picks and to write 8 bytes a row, 4 a pick and 8 an alternative: fp32 rows are bound by that
-// (2^20 x 256 with 8 picks: 1.15 GB in 207 us, 5.6 TB/s; 2^20 x 64: 62 us), rows of the short types and alternatives by the instructions (2^20 x 256 bf16: 118 us for
-// 0.6 GB; fp32 with 8 alternatives 228 us for 1.22 GB).  The gradient reads and writes every logit: 2^23 x 8 116 us, 2^20 x 256 345, 6.3 TB/s.
+// (2^20 x 256 with 8 picks: 1.15 GB in 207 us, 5.6 TB/s; 2^20 x 64: 61 us), rows of the short types and alternatives by the instructions (2^20 x 256 bf16: 112 us for
+// 0.6 GB; with 8 alternatives fp32 226 us for 1.22 GB, bf16 184 for 0.68).  The gradient reads and writes every logit: 2^23 x 8 117 us, 2^20 x 256 348, 6.2 TB/s.
 #include "router_core.hpp"
 
 namespace rs {
@@ -258,7 +258,7 @@ extern "C" int railsched_route_logprobs(const void *logits, int32_t dtype, int64
         };
         // Up to 16 alternatives come from stage 1's lists, in lengths that leave a lane whose whole list is taken as rare: up to eight of rows of more than 32 logits,
         // more of rows of more than 64 (2^20 x 256 with 16: about 700 us by rounds, 302 so).  These kernels are bound by their instructions, most of which a row of
-        // fewer lanes shares among more rows: 2^20 x 256 with 8 takes 237 us with 8 lanes, 254 with 16; bf16 185 and 240; but 2^20 x 128 with 4 lanes half as long again
+        // fewer lanes shares among more rows: 2^20 x 256 with 8 takes 226 us with 8 lanes, 261 with 16; bf16 184 and 240; but 2^20 x 128 with 4 lanes half as long again
         // as with 8.
         if (E > 32 && m > 0 && m <= 8) {
             constexpr std::integral_constant<int, ALT_LISTS_8> lists;

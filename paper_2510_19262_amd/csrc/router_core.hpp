@@ -123,8 +123,8 @@ struct RowRaw {
 };
 // VEC (E >= 4): places of four consecutive experts, interleaved over the lanes, as slot_index() numbers them.  Where E is no multiple of four, the row's last four values stand for
 // the part of a four that it ends with, and are moved to their places when they are taken.  Streaming, but for rows some of whose logits are
-// fetched again (AGAIN): those are to stay in the L2 until then.  Gradient of the distillation of 2^20 x 256: 417 us streaming, 368 so; of the balance
-// loss, which fetches nothing again: 423, 432.
+// fetched again (AGAIN): those are to stay in the L2 until then.  Gradient of the distillation of 2^20 x 256: 386 us streaming, 370 so; of the balance
+// loss, which fetches nothing again: 340, 356.
 template <bool AGAIN, typename T, int LANES, int VPL, bool VEC>
 __device__ __forceinline__ void row_fetch(const T *__restrict__ row, int E, int q, RowRaw<T, VPL, VEC> &raw)
 {
@@ -398,8 +398,9 @@ struct Shape {
 // A kernel that only reads its rows (not WHOLE) takes the fewest lanes that pay: 8 values a lane at least, 16 or 32 of the short types, whose four are
 // half as many bytes.  2^22 x 32: 123 us with 4 lanes, 172 with 8; 2^20 x 64 bf16: 44 with 4, 48 with 8, but fp32 68 and 61; 2^20 x 256 bf16: 118 with 8 lanes,
 // 128 with 16, fp32 205 and 198.  One that writes them too, or keeps sums of its places (WHOLE), is faster with more: gradient of 2^22 x 32: 222 us
-// with 8 lanes, 247 with 4; 2^20 x 64: 95 with 8, 116 with 4.  Read and written one by one: rows of less than four, and where WHOLE short ones that end with a part of a four (gradients
-// of 2^26 logits in rows of 11: 128 us, 142 in fours; of 27: 139 and 131, of 45 bf16: 133 and 88).
+// with 8 lanes, 247 with 4; 2^20 x 64: 95 with 8, 116 with 4.  Read and written one by one: rows of less than four, and where WHOLE rows of 9 to 31
+// that end with a part of a four.  Balance gradient of 2^26 logits, one by one and in fours: bf16 in rows of 9 83 and 114 us, of 17 89 and 118, of 31 60 and 87; fp32 of 9 133 and 136, of 11 127
+// and 141, of 17 134 and 140, but of 14 138 and 115, of 27 136 and 128, of 30 134 and 112; the other gradients and types differ less, the same way.  Longer rows: of 45 bf16 133 and 88.
 template <bool WHOLE, typename T, typename F>
 inline int by_shape(int E, F f)
 {
