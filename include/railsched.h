@@ -377,9 +377,9 @@ int railsched_route_balance_backward(const void *logits, int32_t dtype, int64_t 
  *   loss[r] = tau^2 (sum_j q_j (log q_j - log p[t_idx[j]]) + q_r (log q_r - log p_r))
  * A row without entries has the loss 0 (also with t_lse).  +infinity where q_j > 0 meets an expert that is out.
  * An expert listed twice counts with the sum of its entries' terms.
- * temperature is within 2^-8 .. 2^8: log p - log q, from which loss and gradient are formed, is off by a few 2^-24 of 1 + |logit - t_logit| / tau, while it is itself of
- * order 1 / tau for a large tau.  A gradient is off by about 2^-11 of itself at most at either end where student and teacher differ by about 1; a t_lse counts as the number that it is in
- * fp32 (with a list that leaves p no rest, half a step of t_lse changes the loss by tau^2 times that).
+ * temperature is within 2^-8 .. 2^8: log p - log q, from which loss and gradient are formed, is off by a few 2^-24 of 1 + |logit - t_logit| / tau + |t_lse|, while it is
+ * itself of order 1 / tau for a large tau.  Where student and teacher differ by about 1 that is up to about 2^-11 of a row's gradient at 2^8, and 2^-14 of tau d_loss at 2^-8.  t_lse counts as the
+ * number that it is in fp32 (with a list that leaves p no rest, half a step of t_lse changes the loss by tau^2 times that).
  *   t_idx [rows][K] int32, t_logit [rows][K] fp32, t_lse [rows] fp32 (nullable)  (in; alt_idx and alt_logp of railsched_route_logprobs
  *                                                                                will do, with t_lse = 0 at temperature 1)
  *   loss  [rows] fp32                                                            (out) */

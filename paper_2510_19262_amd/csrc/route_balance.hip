@@ -390,7 +390,7 @@ static Cut balance_cut(int64_t rows, int32_t groups, int E, bool equal)
 }
 // Rows of a workgroup of the gradient: 16 KiB of logits, 32 KiB of rows of more than 256 bytes; whole rounds of the rows in hand; fewer where the GPU would not be full.  Much
 // more is slower by up to a third (2^20 x 256: 340 us with 32 KiB, 417 with 512; 2^21 x 64: 178 with 16, 235 with 256), less pays for the weights too often (2^23 x 8: 135 us
-// with 4 KiB, which one round takes, 90 with 16; 2^20 x 256: 352 with 4).
+// with 4 KiB, the least, a round of the rows in hand, 90 with 16; 2^20 x 256: 352 with 4).
 static int gradient_slice_rows(int64_t rows, int row_bytes, int in_hand)
 {
     int64_t r = (row_bytes <= 256 ? 16384 : 32768) / row_bytes;

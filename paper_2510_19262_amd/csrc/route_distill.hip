@@ -247,9 +247,9 @@ __global__ __launch_bounds__(256) void route_distill_backward_kernel(const T *__
     if (at_row.there && (counts || !add)) row_store<T, LANES, VPL, VEC>(d_logits + (first + threadIdx.x / LANES) * ld_d, E, q0, add != 0, o.y);
 }
 
-// The temperatures that fp32 carries.  d = log p - log q is off by a few 2^-24 times 1 + |logit - t_logit| / tau.  A large tau makes d itself small, of order 1 / tau, so that
+// The temperatures that fp32 carries.  d = log p - log q is off by a few 2^-24 times 1 + |logit - t_logit| / tau + |t_lse|.  A large tau makes d itself small, of order 1 / tau, so that
 // the gradient loses tau 2^-24 of itself; a small one makes that error 2^-24 / tau of q.  Largest errors of 2000 rows of 64 experts, teacher within 0.5 of the student's
-// logits, as a share of a row's gradient: tau 32 7e-5, 256 4e-4, 2^14 2e-2, 10^6 more than all of it; as a share of tau d_loss: 2^-6 1e-5, 2^-8 5e-5, 10^-4 1e-3, 10^-6 0.06.
+// logits, as a share of a row's gradient: tau 32 7e-5, 256 4e-4, 10^4 2e-2, 10^6 more than all of it; as a share of tau d_loss: 2^-6 1e-5, 2^-8 5e-5, 10^-4 1e-3, 10^-6 0.06.
 constexpr float kLeastTau = 0x1p-8f, kMostTau = 0x1p8f;
 
 static int check_distill(int64_t rows, int32_t E, float temperature, const int32_t *t_idx, const float *t_logit, int32_t K)
